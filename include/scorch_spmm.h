@@ -276,6 +276,93 @@ scorch_status_t scorch_dcsr_to_csr_rowptr(int32_t m, int32_t n_stored_rows, cons
                                           const int32_t *row_pos, int32_t *rowptr_out, int32_t *bad_flag,
                                           void *stream);
 
+/*
+ * The two ends of a language model's vocabulary, where a list of token ids meets dense rows.  A batch of token ids is a sparse matrix
+ * with one entry per row; its product with a table is a lookup, its transpose's product the gradient of that table.  A teacher's top
+ * logits are a CSR matrix next to a student's dense ones, and a sequence's history, biases and grammar are lists of ids per row.
+ *
+ * Dense operands are row-major with a row stride (ld...) in elements, of one of the types below; their base needs the alignment of an
+ * element, no more.  Row strides are 64-bit, every offset is computed in 64 bits.  Sums and softmax statistics are held in 32 bits,
+ * results of 16 bits are rounded once, to nearest.  Ids and columns outside [0, vocab) are legal and stand for nothing (padding).  The
+ * order of every sum is fixed, so repeated calls give the same bits.  None of these calls waits or allocates.
+ */
+enum { SCORCH_TYPE_F32 = 0, SCORCH_TYPE_BF16 = 1, SCORCH_TYPE_F16 = 2 };
+
+/*
+ * Lookup:  out[t, j] = scale * E[ids[t], j],  t < tokens, j < d.  E: vocab x d, out: tokens x d, of any two types.  The row of an id outside
+ * [0, vocab) is +0.0.  out must not overlap E or ids.
+ */
+scorch_status_t scorch_embedding_lookup(int32_t tokens, int32_t vocab, int32_t d, const int32_t *ids,
+                                        const void *E, int32_t e_type, int64_t lde, float scale,
+                                        void *out, int32_t out_type, int64_t ldo, void *stream);
+
+/*
+ * Gradient of the table of a lookup:  dE[v, j] = scale * sum over t with ids[t] = v of dout[t, j], for every v < vocab (+0.0 for ids that do not
+ * occur), or, with accumulate != 0, that added to what dE holds; rows of ids that do not occur are then neither read nor written.  The
+ * token positions are sorted by id, so that a row of dE is the sum over a run of them, in ascending order; long runs are cut into pieces whose sums
+ * are added in order.  dout: tokens x d, dE: vocab x d, of any two types; they must not overlap.  workspace (device, 256-byte aligned) of
+ * the size that the function after this one gives (host-only) holds the order and the pieces; executions that share one must not overlap in time.
+ */
+scorch_status_t scorch_embedding_gradient(int32_t tokens, int32_t vocab, int32_t d, const int32_t *ids,
+                                          const void *dout, int32_t dout_type, int64_t lddo, float scale, int32_t accumulate,
+                                          void *dE, int32_t de_type, int64_t ldde,
+                                          void *workspace, size_t workspace_bytes, void *stream);
+scorch_status_t scorch_embedding_gradient_workspace_bytes(int32_t tokens, int32_t vocab, int32_t d, size_t *bytes_out);
+
+/*
+ * Distillation from a teacher's top logits, kept as a CSR matrix of `rows` rows (vals[p]: logit, or log-probability, of column colidx[p]).
+ * With x = 1 / temperature = inv_temperature, for every row i:
+ *
+ *        p_k = exp(x t_k) / sum over the row's stored entries of exp(x t),        q_j = exp(x z_ij) / sum over all columns of exp(x z_i)
+ *        loss_i = sum_k p_k (log p_k - log q_(column of k))                        (Kullback-Leibler divergence)
+ *        d loss_i / d z_ij = x (q_j - sum of p_k over the entries k of column j)
+ *
+ * Z: rows x vocab.  Entries of a row may be in any order and may repeat (every stored entry contributes one term); those with a column
+ * outside [0, vocab) or a value of -infinity count as not stored.  A row without stored entries has loss 0 and a gradient of zeros whatever its
+ * logits are.  Logits of -infinity are columns of probability 0: they have a gradient of -p (0 where the teacher has nothing), and the loss is
+ * +infinity where the teacher has p > 0.  A row of Z that holds nothing else, +infinity or not-a-number has a loss and a gradient that are not numbers.  inv_temperature must be positive and finite.
+ *
+ * scorch_distill_loss writes loss[rows] and stats[rows][2], the largest logit of each row of Z and the sum of exp(x (z - largest));
+ * scorch_distill_gradient takes these stats and writes dZ (rows x vocab, of Z's type), row i times dloss[i]; scorch_distill_loss_gradient does
+ * both at once, for a dloss known beforehand (a mean's 1 / rows, say).  dloss == NULL: ones.  dZ may be Z itself (with the same row
+ * stride) and must not overlap anything otherwise.  The gradient calls take up to SCORCH_DISTILL_VOCAB_MAX columns (SCORCH_ERR_UNSUPPORTED).
+ */
+#define SCORCH_DISTILL_VOCAB_MAX 524288
+scorch_status_t scorch_distill_loss(int32_t rows, int32_t vocab, const void *Z, int32_t z_type, int64_t ldz,
+                                    const int32_t *rowptr, const int32_t *colidx, const float *vals, float inv_temperature,
+                                    float *loss, float *stats, void *stream);
+scorch_status_t scorch_distill_gradient(int32_t rows, int32_t vocab, const void *Z, int32_t z_type, int64_t ldz,
+                                        const int32_t *rowptr, const int32_t *colidx, const float *vals, float inv_temperature,
+                                        const float *stats, const float *dloss, void *dZ, int64_t lddz, void *stream);
+scorch_status_t scorch_distill_loss_gradient(int32_t rows, int32_t vocab, const void *Z, int32_t z_type, int64_t ldz,
+                                             const int32_t *rowptr, const int32_t *colidx, const float *vals, float inv_temperature,
+                                             const float *dloss, float *loss, void *dZ, int64_t lddz, void *stream);
+
+/*
+ * Logits of the next token, before it is chosen.  For every row i and column j, with x = logits[i, j]:
+ *
+ *        if j occurs in the row's history:                  x = x > 0 ? x / repetition[i] : x * repetition[i]
+ *        x = x - frequency[i] * c - (c > 0 ? presence[i] : 0)        c: how often j occurs in it from position generated_from[i] on
+ *        x = x + the row's bias entries of column j, added up in their order
+ *        if the row's mask forbids j:                       x = -infinity
+ *
+ * All of it in 32 bits, rounded once to the type of out.  What is NULL is left out: histories and biases are CSR lists (rowptr: int32[rows + 1];
+ * tokens outside [0, vocab) count for nothing; tokens may repeat), the penalties are one float per row, generated_from one position per row,
+ * counted from the row's first history entry (NULL: 0, everything was generated).  mask: one bit per column, bit j % 32 of word j / 32
+ * of the row, 1 = allowed; rows of ldm >= ceil(vocab / 32) words.  A row whose mask allows nothing comes out as -infinity throughout.
+ * out: rows x vocab, of any type; it may be logits itself (same type and row stride) and must not overlap anything otherwise.
+ */
+typedef struct scorch_logits_rules {
+    const int32_t *history_rowptr, *history, *generated_from;
+    const float *repetition, *presence, *frequency;
+    const int32_t *bias_rowptr, *bias_tokens;
+    const float *bias_vals;
+    const uint32_t *mask;
+    int64_t ldm;
+} scorch_logits_rules_t;
+scorch_status_t scorch_logits_process(int32_t rows, int32_t vocab, const void *logits, int32_t type, int64_t ldl,
+                                      const scorch_logits_rules_t *rules, void *out, int32_t out_type, int64_t ldo, void *stream);
+
 /* (Plumbing; no counterpart in the paper.)  Static text for a status code. */
 const char *scorch_status_string(scorch_status_t status);
 

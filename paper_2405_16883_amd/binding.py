@@ -27,6 +27,8 @@ EXPORTS = (
     "scorch_spmm_plan_destroy", "scorch_spmm_plan_info", "scorch_status_string", "scorch_last_error",
     "scorch_sddmm_csr", "scorch_sddmm_csr_planned", "scorch_spmm_csr_planned_epilogue", "scorch_coo_to_csr_rowptr",
     "scorch_dcsr_to_csr_rowptr", "scorch_spmm_csr_static", "scorch_dense_layer",
+    "scorch_embedding_lookup", "scorch_embedding_gradient", "scorch_embedding_gradient_workspace_bytes",
+    "scorch_distill_loss", "scorch_distill_gradient", "scorch_distill_loss_gradient", "scorch_logits_process",
 )
 
 
@@ -48,6 +50,13 @@ class PlanInfo(ctypes.Structure):
         ("off_split", ctypes.c_uint64), ("off_partials", ctypes.c_uint64), ("workspace_bytes_used", ctypes.c_uint64),
         ("n_hot_columns", ctypes.c_int32), ("hot_share", ctypes.c_float), ("off_wave_span", ctypes.c_uint64), ("off_win_stage", ctypes.c_uint64),
     ]
+
+
+class LogitsRules(ctypes.Structure):
+    """scorch_logits_rules_t: device pointers, or None for what is left out."""
+    _fields_ = [(name, ctypes.c_void_p) for name in (
+        "history_rowptr", "history", "generated_from", "repetition", "presence", "frequency", "bias_rowptr", "bias_tokens", "bias_vals",
+        "mask")] + [("ldm", ctypes.c_int64)]
 
 
 _lib = None
@@ -90,6 +99,21 @@ def load_library() -> ctypes.CDLL:
     lib.scorch_sddmm_csr_planned.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, i32, vp, vp]
     lib.scorch_dense_layer.restype = i32
     lib.scorch_dense_layer.argtypes = [i32, i32, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp]
+    f32 = ctypes.c_float
+    lib.scorch_embedding_lookup.restype = i32
+    lib.scorch_embedding_lookup.argtypes = [i32, i32, i32, vp, vp, i32, i64, f32, vp, i32, i64, vp]
+    lib.scorch_embedding_gradient.restype = i32
+    lib.scorch_embedding_gradient.argtypes = [i32, i32, i32, vp, vp, i32, i64, f32, i32, vp, i32, i64, vp, ctypes.c_size_t, vp]
+    lib.scorch_embedding_gradient_workspace_bytes.restype = i32
+    lib.scorch_embedding_gradient_workspace_bytes.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.scorch_distill_loss.restype = i32
+    lib.scorch_distill_loss.argtypes = [i32, i32, vp, i32, i64, vp, vp, vp, f32, vp, vp, vp]
+    lib.scorch_distill_gradient.restype = i32
+    lib.scorch_distill_gradient.argtypes = [i32, i32, vp, i32, i64, vp, vp, vp, f32, vp, vp, vp, i64, vp]
+    lib.scorch_distill_loss_gradient.restype = i32
+    lib.scorch_distill_loss_gradient.argtypes = [i32, i32, vp, i32, i64, vp, vp, vp, f32, vp, vp, vp, i64, vp]
+    lib.scorch_logits_process.restype = i32
+    lib.scorch_logits_process.argtypes = [i32, i32, vp, i32, i64, ctypes.POINTER(LogitsRules), vp, i32, i64, vp]
     lib.scorch_status_string.restype = ctypes.c_char_p
     lib.scorch_status_string.argtypes = [i32]
     lib.scorch_last_error.restype = ctypes.c_char_p
@@ -275,3 +299,77 @@ def scorch_dcsr_to_csr_rowptr(m: int, row_ids: torch.Tensor, row_pos: torch.Tens
     _check(lib.scorch_dcsr_to_csr_rowptr(m, row_ids.numel(), _dev_ptr(row_ids, torch.int32, "row_ids"),
                                          row_pos.data_ptr(), _dev_ptr(rowptr_out, torch.int32, "rowptr_out"),
                                          _dev_ptr(bad_flag, torch.int32, "bad_flag"), _stream_handle(stream)))
+
+
+def scorch_embedding_lookup(ids: torch.Tensor, E: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+                            stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out[t] = scale * E[ids[t]]; rows of ids outside the table (padding) become zeros.  E and out: float32, bfloat16 or float16."""
+    st = (_native or _load_native()).embedding_lookup(ids, E, out, scale, stream)
+    if st:
+        _check(st)
+
+
+def scorch_embedding_gradient_workspace_bytes(tokens: int, vocab: int, d: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().scorch_embedding_gradient_workspace_bytes(tokens, vocab, d, ctypes.byref(out)))
+    return int(out.value)
+
+
+def scorch_embedding_gradient(ids: torch.Tensor, dout: torch.Tensor, dE: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+                              workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """dE[v] = scale * sum of the rows of dout whose id is v, or that added to dE.  ``workspace`` (uint8, GPU) is allocated with torch
+    for the stream of the call if not given."""
+    if workspace is None:
+        size = scorch_embedding_gradient_workspace_bytes(dout.shape[0], dE.shape[0], dE.shape[1])
+        if stream is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dE.device)
+        else:
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(size, dtype=torch.uint8, device=dE.device)
+    st = (_native or _load_native()).embedding_gradient(ids, dout, dE, scale, int(accumulate), workspace, stream)
+    if st:
+        _check(st)
+
+
+DISTILL_VOCAB_MAX = 524288
+
+
+def scorch_distill_loss(Z: torch.Tensor, rowptr: torch.Tensor, colidx: torch.Tensor, vals: torch.Tensor, inv_temperature: float,
+                        loss: torch.Tensor, stats: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """loss[i]: divergence of softmax(inv_temperature * Z[i]) from the softmax over the teacher's stored logits of row i (CSR);
+    stats[i]: the largest logit and the sum of exponentials relative to it, for scorch_distill_gradient."""
+    st = (_native or _load_native()).distill_loss(Z, rowptr, colidx, vals, inv_temperature, loss, stats, stream)
+    if st:
+        _check(st)
+
+
+def scorch_distill_gradient(Z: torch.Tensor, rowptr: torch.Tensor, colidx: torch.Tensor, vals: torch.Tensor, inv_temperature: float,
+                            stats: torch.Tensor, dloss: Optional[torch.Tensor], dZ: torch.Tensor,
+                            stream: Optional[torch.cuda.Stream] = None) -> None:
+    """dZ = gradient of sum(dloss * loss) by Z (dloss may be None: ones).  dZ may be Z."""
+    st = (_native or _load_native()).distill_gradient(Z, rowptr, colidx, vals, inv_temperature, stats, dloss, dZ, stream)
+    if st:
+        _check(st)
+
+
+def scorch_distill_loss_gradient(Z: torch.Tensor, rowptr: torch.Tensor, colidx: torch.Tensor, vals: torch.Tensor, inv_temperature: float,
+                                 dloss: Optional[torch.Tensor], loss: torch.Tensor, dZ: torch.Tensor,
+                                 stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Loss and gradient in one pass, for a dloss that is known beforehand.  dZ may be Z."""
+    st = (_native or _load_native()).distill_loss_gradient(Z, rowptr, colidx, vals, inv_temperature, dloss, loss, dZ, stream)
+    if st:
+        _check(st)
+
+
+def scorch_logits_process(logits: torch.Tensor, out: torch.Tensor, history_rowptr: Optional[torch.Tensor] = None,
+                          history: Optional[torch.Tensor] = None, generated_from: Optional[torch.Tensor] = None,
+                          repetition: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                          frequency: Optional[torch.Tensor] = None, bias_rowptr: Optional[torch.Tensor] = None,
+                          bias_tokens: Optional[torch.Tensor] = None, bias_vals: Optional[torch.Tensor] = None,
+                          mask: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out = logits after penalties for the tokens of each row's history (CSR), biases (CSR) and a grammar mask (int32 words, a bit per
+    column, 1 = allowed).  out may be logits."""
+    st = (_native or _load_native()).logits_process(logits, out, history_rowptr, history, generated_from, repetition, presence, frequency,
+                                                    bias_rowptr, bias_tokens, bias_vals, mask, stream)
+    if st:
+        _check(st)

@@ -10,6 +10,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <cstdint>
 #include <exception>
 
 #include "scorch_spmm.h"
@@ -42,7 +43,7 @@ struct Args {
             ok = false;
         } else if (t.scalar_type() != type) {
             PyObject *got = PyObject_GetAttrString(v[i], "dtype");
-            if (got) PyErr_Format(PyExc_ValueError, "%s must be %s, got %S", name, type == at::kInt ? "torch.int32" : "torch.float32", got);
+            if (got) PyErr_Format(PyExc_ValueError, "%s must be %s, got %S", name, type == at::kInt ? "torch.int32" : type == at::kByte ? "torch.uint8" : "torch.float32", got);
             Py_XDECREF(got);
             ok = false;
         }
@@ -66,6 +67,69 @@ struct Args {
             return 0;
         }
         return (int32_t)(t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1)));
+    }
+
+    // A list of n int32 (or float) without gaps on the current device; n < 0: of any length, which is put there.  None: nullptr if that is
+    // allowed.
+    void *list(int i, at::ScalarType type, const char *name, int64_t &n, bool optional = false) {
+        if (ok && v[i] == Py_None && !optional) fail(PyExc_TypeError, "%s must be a tensor", name);
+        if (!ok || v[i] == Py_None) return nullptr;
+        void *p = ptr(i, type, name);
+        if (!ok) return nullptr;
+        const at::Tensor &t = THPVariable_Unpack(v[i]);
+        if (!t.is_contiguous()) fail(PyExc_ValueError, "%s must be contiguous", name);
+        else if (t.numel() > INT32_MAX) fail(PyExc_ValueError, "%s has too many elements", name);
+        else if (n >= 0 && t.numel() != n) PyErr_Format(PyExc_ValueError, "%s must have %lld elements, got %lld", name, (long long)n, (long long)t.numel()), ok = false;
+        else if (t.get_device() != c10::hip::current_device()) fail(PyExc_ValueError, "%s must live on the current device", name);
+        n = t.numel();
+        return ok ? p : nullptr;
+    }
+    int32_t *int_list(int i, const char *name, int64_t n, bool optional = false) {
+        return static_cast<int32_t *>(list(i, at::kInt, name, n, optional));
+    }
+    float *float_list(int i, const char *name, int64_t n, bool optional = false) {
+        return static_cast<float *>(list(i, at::kFloat, name, n, optional));
+    }
+
+    // A matrix of 32- or 16-bit floats with contiguous rows on the current device.
+    struct Matrix {
+        void *p = nullptr;
+        int32_t type = 0, rows = 0, cols = 0;
+        int64_t ld = 0;
+    };
+    Matrix matrix(int i, const char *name) {
+        Matrix m;
+        if (!ok) return m;
+        if (!THPVariable_Check(v[i])) {
+            fail(PyExc_TypeError, "%s must be a tensor", name);
+            return m;
+        }
+        const at::Tensor &t = THPVariable_Unpack(v[i]);
+        if (!t.is_cuda()) fail(PyExc_ValueError, "%s must live on the GPU", name);
+        else if (t.scalar_type() == at::kFloat) m.type = SCORCH_TYPE_F32;
+        else if (t.scalar_type() == at::kBFloat16) m.type = SCORCH_TYPE_BF16;
+        else if (t.scalar_type() == at::kHalf) m.type = SCORCH_TYPE_F16;
+        else fail(PyExc_ValueError, "%s must be float32, bfloat16 or float16", name);
+        if (!ok) return m;
+        if (t.dim() != 2 || (t.numel() > 0 && t.size(1) > 1 && t.stride(1) != 1)) fail(PyExc_ValueError, "%s must be 2-D with unit column stride", name);
+        else if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX) fail(PyExc_ValueError, "%s has too many rows or columns", name);
+        else if (t.get_device() != c10::hip::current_device()) fail(PyExc_ValueError, "%s must live on the current device", name);
+        if (!ok) return m;
+        m.rows = (int32_t)t.size(0);
+        m.cols = (int32_t)t.size(1);
+        m.ld = t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
+        m.p = t.numel() > 0 ? t.data_ptr() : nullptr;
+        return m;
+    }
+    float number(int i) {
+        if (!ok) return 0.f;
+        const double x = PyFloat_AsDouble(v[i]);
+        if (x == -1.0 && PyErr_Occurred()) ok = false;
+        return (float)x;
+    }
+    void fail(PyObject *error, const char *text, const char *name = "") {
+        PyErr_Format(error, text, name);
+        ok = false;
     }
 
     // stream: None for the current stream of the current device
@@ -220,6 +284,131 @@ PyObject *coo_to_csr_rowptr(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
     return status_of(a, [&] { return scorch_coo_to_csr_rowptr(m, nnz, rows, out, bad, s); });
 }
 
+// (ids, E, out, scale, stream)
+PyObject *embedding_lookup(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+    if (!count_is(nargs, 5)) return nullptr;
+    Args a{v};
+    const auto E = a.matrix(1, "E"), out = a.matrix(2, "out");
+    const int32_t *ids = a.int_list(0, "ids", out.rows);
+    const float scale = a.number(3);
+    void *s = a.stream(4);
+    if (a.ok && E.cols != out.cols) a.fail(PyExc_ValueError, "E and out have different numbers of columns");
+    return status_of(a, [&] { return scorch_embedding_lookup(out.rows, E.rows, E.cols, ids, E.p, E.type, E.ld, scale, out.p, out.type, out.ld, s); });
+}
+
+// (ids, dout, dE, scale, accumulate, workspace, stream)
+PyObject *embedding_gradient(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+    if (!count_is(nargs, 7)) return nullptr;
+    Args a{v};
+    const auto dout = a.matrix(1, "dout"), dE = a.matrix(2, "dE");
+    const int32_t *ids = a.int_list(0, "ids", dout.rows);
+    const float scale = a.number(3);
+    const int32_t accumulate = a.i32(4);
+    int64_t bytes = -1;
+    void *ws = a.list(5, at::kByte, "workspace", bytes);
+    void *s = a.stream(6);
+    if (a.ok && dout.cols != dE.cols) a.fail(PyExc_ValueError, "dout and dE have different numbers of columns");
+    return status_of(a, [&] {
+        return scorch_embedding_gradient(dout.rows, dE.rows, dE.cols, ids, dout.p, dout.type, dout.ld, scale, accumulate, dE.p, dE.type, dE.ld, ws,
+                                         (size_t)bytes, s);
+    });
+}
+
+// The teacher's CSR matrix: arguments i, i + 1, i + 2.
+struct Teacher {
+    const int32_t *rowptr, *colidx;
+    const float *vals;
+    Teacher(Args &a, int i, int64_t rows) {
+        rowptr = a.int_list(i, "rowptr", rows + 1);
+        int64_t nnz = -1;
+        colidx = static_cast<int32_t *>(a.list(i + 1, at::kInt, "colidx", nnz));
+        vals = a.float_list(i + 2, "vals", nnz);
+    }
+};
+
+// (Z, rowptr, colidx, vals, inv_temperature, loss, stats, stream)
+PyObject *distill_loss(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+    if (!count_is(nargs, 8)) return nullptr;
+    Args a{v};
+    const auto Z = a.matrix(0, "Z");
+    const Teacher t(a, 1, Z.rows);
+    const float x = a.number(4);
+    float *loss = a.float_list(5, "loss", Z.rows), *stats = a.float_list(6, "stats", 2 * (int64_t)Z.rows);
+    void *s = a.stream(7);
+    return status_of(a, [&] { return scorch_distill_loss(Z.rows, Z.cols, Z.p, Z.type, Z.ld, t.rowptr, t.colidx, t.vals, x, loss, stats, s); });
+}
+
+bool same_kind(Args &a, const Args::Matrix &Z, const Args::Matrix &dZ) {
+    if (a.ok && (dZ.rows != Z.rows || dZ.cols != Z.cols || dZ.type != Z.type)) a.fail(PyExc_ValueError, "dZ must have the shape and type of Z");
+    return a.ok;
+}
+
+// (Z, rowptr, colidx, vals, inv_temperature, stats, dloss, dZ, stream)
+PyObject *distill_gradient(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+    if (!count_is(nargs, 9)) return nullptr;
+    Args a{v};
+    const auto Z = a.matrix(0, "Z"), dZ = a.matrix(7, "dZ");
+    const Teacher t(a, 1, Z.rows);
+    const float x = a.number(4);
+    const float *stats = a.float_list(5, "stats", 2 * (int64_t)Z.rows), *dloss = a.float_list(6, "dloss", Z.rows, true);
+    void *s = a.stream(8);
+    if (!same_kind(a, Z, dZ)) return nullptr;
+    return status_of(a, [&] {
+        return scorch_distill_gradient(Z.rows, Z.cols, Z.p, Z.type, Z.ld, t.rowptr, t.colidx, t.vals, x, stats, dloss, dZ.p, dZ.ld, s);
+    });
+}
+
+// (Z, rowptr, colidx, vals, inv_temperature, dloss, loss, dZ, stream)
+PyObject *distill_loss_gradient(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+    if (!count_is(nargs, 9)) return nullptr;
+    Args a{v};
+    const auto Z = a.matrix(0, "Z"), dZ = a.matrix(7, "dZ");
+    const Teacher t(a, 1, Z.rows);
+    const float x = a.number(4);
+    const float *dloss = a.float_list(5, "dloss", Z.rows, true);
+    float *loss = a.float_list(6, "loss", Z.rows);
+    void *s = a.stream(8);
+    if (!same_kind(a, Z, dZ)) return nullptr;
+    return status_of(a, [&] {
+        return scorch_distill_loss_gradient(Z.rows, Z.cols, Z.p, Z.type, Z.ld, t.rowptr, t.colidx, t.vals, x, dloss, loss, dZ.p, dZ.ld, s);
+    });
+}
+
+// (logits, out, history_rowptr, history, generated_from, repetition, presence, frequency, bias_rowptr, bias_tokens, bias_vals, mask, stream)
+PyObject *logits_process(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
+    if (!count_is(nargs, 13)) return nullptr;
+    Args a{v};
+    const auto x = a.matrix(0, "logits"), out = a.matrix(1, "out");
+    scorch_logits_rules_t r{};
+    int64_t any = -1;
+    if (a.ok && (v[2] == Py_None) != (v[3] == Py_None)) a.fail(PyExc_ValueError, "history_rowptr and history belong together");
+    r.history_rowptr = a.int_list(2, "history_rowptr", (int64_t)x.rows + 1, true);
+    r.history = static_cast<int32_t *>(a.list(3, at::kInt, "history", any, true));
+    r.generated_from = a.int_list(4, "generated_from", x.rows, true);
+    r.repetition = a.float_list(5, "repetition", x.rows, true);
+    r.presence = a.float_list(6, "presence", x.rows, true);
+    r.frequency = a.float_list(7, "frequency", x.rows, true);
+    if (a.ok && ((v[8] == Py_None) != (v[9] == Py_None) || (v[8] == Py_None) != (v[10] == Py_None)))
+        a.fail(PyExc_ValueError, "bias_rowptr, bias_tokens and bias_vals belong together");
+    r.bias_rowptr = a.int_list(8, "bias_rowptr", (int64_t)x.rows + 1, true);
+    int64_t entries = -1;
+    r.bias_tokens = static_cast<int32_t *>(a.list(9, at::kInt, "bias_tokens", entries, true));
+    r.bias_vals = a.float_list(10, "bias_vals", entries, true);
+    if (a.ok && v[11] != Py_None) {
+        r.mask = reinterpret_cast<const uint32_t *>(a.ints(11, "mask"));
+        const int64_t ld = a.ld(11, "mask");
+        if (a.ok) {
+            const at::Tensor &m = THPVariable_Unpack(v[11]);
+            if (m.size(0) != x.rows || m.size(1) < ((int64_t)x.cols + 31) / 32) a.fail(PyExc_ValueError, "mask must have a row per row of logits and a bit per column");
+            else if (m.get_device() != c10::hip::current_device()) a.fail(PyExc_ValueError, "%s must live on the current device", "mask");
+        }
+        r.ldm = ld;
+    }
+    void *s = a.stream(12);
+    if (a.ok && (out.rows != x.rows || out.cols != x.cols)) a.fail(PyExc_ValueError, "out must have the shape of logits");
+    return status_of(a, [&] { return scorch_logits_process(x.rows, x.cols, x.p, x.type, x.ld, &r, out.p, out.type, out.ld, s); });
+}
+
 // What the interpreter calls.  A tensor without plain memory (sparse, fake, wrapped by a transform) and a missing GPU make torch
 // throw; the exception becomes a Python error here, it must not reach the interpreter's C frames.
 typedef PyObject *(*method)(PyObject *, PyObject *const *, Py_ssize_t);
@@ -244,6 +433,12 @@ PyMethodDef kMethods[] = {
     entry<sddmm_planned>("sddmm_csr_planned"),
     entry<dense_layer>("dense_layer"),
     entry<coo_to_csr_rowptr>("coo_to_csr_rowptr"),
+    entry<embedding_lookup>("embedding_lookup"),
+    entry<embedding_gradient>("embedding_gradient"),
+    entry<distill_loss>("distill_loss"),
+    entry<distill_gradient>("distill_gradient"),
+    entry<distill_loss_gradient>("distill_loss_gradient"),
+    entry<logits_process>("logits_process"),
     {nullptr, nullptr, 0, nullptr},
 };
 

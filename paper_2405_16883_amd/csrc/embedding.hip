@@ -1,0 +1,525 @@
+// Lookup of rows by token id, and the gradient of the table it reads.
+//
+// Lookup: out[t, :] = scale E[ids[t], :].  A copy with a gather in front: bound by the bytes of the rows read and written.  A group of
+// lanes takes a row, 16 bytes of the wider type per lane and step, and several rows at a time, so that their loads are in flight together.
+//
+// Gradient: dE[v, :] = scale * sum of the rows dout[t, :] with ids[t] = v.  Bound by the bytes of dout and dE.  Few ids make up much of a
+// text, so rows of dE differ in work by orders of magnitude: the token positions are sorted by id and the sorted list is cut into chunks
+// of equal length, whatever the runs in it.  A wavefront walks a chunk of a tile of columns with the sum of the current run in registers;
+// runs that end where they began are stored, those that cross a border leave partial rows, which a second launch adds in order.  No
+// floating-point atomics: the order of every sum is that of the token positions.
+#include "device_util.h"
+#include "vocab_util.h"
+
+#include <algorithm>
+
+namespace scorch {
+
+// ------------------------------------------------------------------------------------------
+// lookup
+// ------------------------------------------------------------------------------------------
+struct LookupArgs {
+    const int32_t *ids;
+    const void *E;
+    void *out;
+    int64_t lde, ldo;
+    int32_t tokens, vocab, d;
+    int32_t lanes;  // lanes per row, a power of two
+    float scale;
+};
+
+constexpr int kLookupRows = 4;  // rows a group has in flight
+
+template <typename TE, typename TO>
+__global__ __launch_bounds__(kBlock) void lookup_kernel(const LookupArgs a) {
+    constexpr int N = kPer16<TE, TO>;
+    const int groups = kBlock / a.lanes;
+    const int group = (int)threadIdx.x / a.lanes, lane = (int)threadIdx.x % a.lanes;
+    const int64_t t0 = ((int64_t)blockIdx.x * groups + group) * kLookupRows;
+    const int c0 = ((int)blockIdx.y * a.lanes + lane) * N;
+    if (c0 >= a.d) return;
+    const int left = a.d - c0;
+    const TE *src[kLookupRows];
+    bool there[kLookupRows];
+#pragma unroll
+    for (int i = 0; i < kLookupRows; ++i) {
+        const int32_t id = t0 + i < a.tokens ? a.ids[t0 + i] : -1;
+        there[i] = id >= 0 && id < a.vocab;
+        src[i] = static_cast<const TE *>(a.E) + (int64_t)(there[i] ? id : 0) * a.lde + c0;
+    }
+    float x[kLookupRows][N];
+#pragma unroll
+    for (int i = 0; i < kLookupRows; ++i) {
+        if (!there[i]) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[i][j] = 0.f;
+        } else if (left >= N) {
+            load_floats(src[i], x[i]);
+        } else {
+            load_floats_part(src[i], left, 0.f, x[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kLookupRows; ++i) {
+        if (t0 + i >= a.tokens) break;
+        if (there[i])
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[i][j] *= a.scale;
+        TO *dst = static_cast<TO *>(a.out) + (t0 + i) * a.ldo + c0;
+        if (left >= N) store_floats(dst, x[i]);
+        else store_floats_part(dst, left, x[i]);
+    }
+}
+
+scorch_status_t launch_lookup(int32_t tokens, int32_t vocab, int32_t d, const int32_t *ids, const void *E, int32_t e_type, int64_t lde,
+                              float scale, void *out, int32_t out_type, int64_t ldo, hipStream_t stream) {
+    LookupArgs a{ids, E, out, lde, ldo, tokens, vocab, d, 1, scale};
+    bool ok = true, fits = true;
+    ok = with_type(e_type, [&](auto te) {
+             ok = with_type(out_type, [&](auto to) {
+                 typedef typename decltype(te)::type TE;
+                 typedef typename decltype(to)::type TO;
+                 const int64_t vectors = ((int64_t)d + kPer16<TE, TO> - 1) / kPer16<TE, TO>;
+                 while (a.lanes < kBlock && a.lanes < vectors) a.lanes *= 2;
+                 const int64_t rows = (int64_t)(kBlock / a.lanes) * kLookupRows;
+                 const int64_t blocks = (tokens + rows - 1) / rows;
+                 fits = grid_fits(blocks, kBlock);
+                 if (fits)
+                     hipLaunchKernelGGL((lookup_kernel<TE, TO>), dim3((uint32_t)blocks, (uint32_t)((vectors + a.lanes - 1) / a.lanes)),
+                                        dim3(kBlock), 0, stream, a);
+             });
+         }) && ok;
+    if (!ok) {
+        set_error("embedding lookup: unknown type (%d, %d)", e_type, out_type);
+        return SCORCH_ERR_INVALID_ARG;
+    }
+    if (!fits) {
+        set_error("embedding lookup: %d tokens need a larger launch than HIP takes", tokens);
+        return SCORCH_ERR_UNSUPPORTED;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "launch lookup_kernel");
+    return SCORCH_OK;
+}
+
+// ------------------------------------------------------------------------------------------
+// gradient: token positions sorted by id
+// ------------------------------------------------------------------------------------------
+// A stable radix sort from the lowest digit up, of digits wide enough that two passes do for a vocabulary of a million.  A pass is two
+// launches: every workgroup counts the digits of its part of the list, then finds where they go from all counts and moves its part.
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / kWave;
+constexpr int kDigitBits = 10;
+constexpr int kBins = 1 << kDigitBits;
+constexpr int kSortRounds = 8;                           // ids per lane and step
+constexpr int kSortStep = kSortThreads * kSortRounds;
+constexpr int kSortParts = 128;                          // workgroups at most
+
+struct SortArgs {
+    const int32_t *keys_in, *perm_in;  // perm_in == nullptr: the first pass, the position itself, and keys_in are the caller's ids
+    int32_t *keys_out, *perm_out;
+    int32_t *counts;                   // [parts][kBins]
+    int32_t tokens, vocab;
+    int32_t parts, part_len;           // a multiple of kSortStep
+    int32_t shift, bits;
+};
+
+// Ids outside the table become `vocab`: sorted behind all others.
+__device__ __forceinline__ int32_t sort_key(const SortArgs &a, int64_t i) {
+    const int32_t k = a.keys_in[i];
+    return !a.perm_in && (uint32_t)k >= (uint32_t)a.vocab ? a.vocab : k;
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a) {
+    __shared__ int32_t s_count[kBins];
+    s_count[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t begin = (int64_t)blockIdx.x * a.part_len;
+    const int64_t end = std::min<int64_t>(begin + a.part_len, a.tokens);
+    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads)
+        atomicAdd(&s_count[(sort_key(a, i) >> a.shift) & ((1 << a.bits) - 1)], 1);
+    __syncthreads();
+    a.counts[(int64_t)blockIdx.x * kBins + threadIdx.x] = s_count[threadIdx.x];
+}
+
+// The lanes of this wavefront that hold the same digit, of those that take part.
+__device__ __forceinline__ uint64_t same_digit(int digit, int bits, bool valid) {
+    uint64_t peers = __ballot(valid);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot(digit >> b & 1);
+        peers &= digit >> b & 1 ? set : ~set;
+    }
+    return peers;
+}
+
+// Exclusive sum over the threads of a workgroup of kSortThreads.
+__device__ __forceinline__ int32_t sort_scan(int32_t x, int32_t *s_wave) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    int32_t sum = x;
+#pragma unroll
+    for (int o = 1; o < kWave; o *= 2) {
+        const int32_t y = __shfl_up(sum, o);
+        if (lane >= o) sum += y;
+    }
+    if (lane == 63) s_wave[wv] = sum;
+    __syncthreads();
+    int32_t before = 0;
+    for (int w = 0; w < wv; ++w) before += s_wave[w];
+    __syncthreads();
+    return before + sum - x;
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs a) {
+    __shared__ int32_t s_base[kBins];                // where the next id of a digit goes
+    __shared__ int32_t s_count[kSortWaves][kBins];   // of this step, per wavefront; then the wavefront's first place
+    __shared__ int32_t s_wave[kSortWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    int32_t before = 0, total = 0;
+    for (int p = 0; p < a.parts; ++p) {
+        const int32_t c = a.counts[(int64_t)p * kBins + tid];
+        if (p < (int)blockIdx.x) before += c;
+        total += c;
+    }
+    s_base[tid] = sort_scan(total, s_wave) + before;
+
+    const int64_t begin = (int64_t)blockIdx.x * a.part_len;
+    const int64_t end = std::min<int64_t>(begin + a.part_len, a.tokens);
+    for (int64_t step = begin; step < end; step += kSortStep) {
+        for (int i = tid; i < kSortWaves * kBins; i += kSortThreads) (&s_count[0][0])[i] = 0;
+        __syncthreads();
+        int32_t key[kSortRounds], place[kSortRounds];
+        const int64_t mine = step + (int64_t)wv * kWave * kSortRounds + lane;  // a wavefront has consecutive positions
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            const int64_t i = mine + r * kWave;
+            const bool valid = i < end;
+            key[r] = valid ? sort_key(a, i) : 0;
+        }
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            const bool valid = mine + r * kWave < end;
+            const int digit = key[r] >> a.shift & ((1 << a.bits) - 1);
+            const uint64_t peers = same_digit(digit, a.bits, valid);
+            place[r] = s_count[wv][digit] + __popcll(peers & ((1ull << lane) - 1));
+            wave_lds_sync();
+            if (valid && (peers >> lane) == 1) s_count[wv][digit] = place[r] + 1;  // the last of the peers
+            wave_lds_sync();
+        }
+        __syncthreads();
+        {
+            int32_t at = s_base[tid];
+            for (int w = 0; w < kSortWaves; ++w) {
+                const int32_t c = s_count[w][tid];
+                s_count[w][tid] = at;
+                at += c;
+            }
+            s_base[tid] = at;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            const int64_t i = mine + r * kWave;
+            if (i < end) {
+                const int digit = key[r] >> a.shift & ((1 << a.bits) - 1);
+                const int32_t to = s_count[wv][digit] + place[r];
+                a.keys_out[to] = key[r];
+                a.perm_out[to] = a.perm_in ? a.perm_in[i] : (int32_t)i;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// gradient: sums of runs
+// ------------------------------------------------------------------------------------------
+struct RunArgs {
+    const int32_t *keys, *perm;  // sorted by id
+    const void *dout;
+    void *dE;
+    float *partials;             // [chunks][2][stride]: the run a chunk begins with, if it began before; the run it ends with, if it goes on and began here
+    int64_t lddo, ldde;
+    int32_t tokens, vocab, d;
+    int32_t chunk, chunks;       // entries per chunk
+    int32_t tiles;               // tiles of columns
+    int64_t stride;              // of the partial rows
+    int64_t reduce_blocks;       // workgroups of the sums; the others store zeros
+    float scale;
+    int32_t accumulate;
+};
+
+constexpr int kGradLoads = 8;  // rows of dout in flight per wavefront
+constexpr int kFillRows = 64;  // rows of dE a wavefront looks at for ones without a token
+
+template <typename TD, typename TE, int N>
+__device__ __forceinline__ void store_row(const RunArgs &a, int32_t id, int c0, int left, const float (&acc)[N]) {
+    TE *dst = static_cast<TE *>(a.dE) + (int64_t)id * a.ldde + c0;
+    float y[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) y[j] = acc[j] * a.scale;
+    if (left >= N) {
+        if (a.accumulate) {
+            float old[N];
+            load_floats(dst, old);
+#pragma unroll
+            for (int j = 0; j < N; ++j) y[j] += old[j];
+        }
+        store_floats(dst, y);
+    } else {
+        if (a.accumulate)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (j < left) y[j] += (float)dst[j];
+        store_floats_part(dst, left, y);
+    }
+}
+
+// First place in the sorted list with an id of at least `id`.
+__device__ __forceinline__ int32_t first_of(const int32_t *keys, int32_t n, int32_t id) {
+    int32_t lo = 0, len = n;
+    while (len > 0) {
+        const int32_t half = len >> 1;
+        if (keys[lo + half] < id) {
+            lo += half + 1;
+            len -= half + 1;
+        } else {
+            len = half;
+        }
+    }
+    return lo;
+}
+
+template <typename TD, typename TE>
+__global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
+    constexpr int N = 16 / sizeof(TD);
+    const int lane = threadIdx.x & 63;
+    if ((int64_t)blockIdx.x >= a.reduce_blocks) {
+        // rows without a token become zeros: a lane looks one id up, then the wavefront stores row by row
+        const int64_t v0 = (((int64_t)blockIdx.x - a.reduce_blocks) * kWavesPerBlock + (threadIdx.x >> 6)) * kFillRows;
+        const int64_t v = v0 + lane;
+        bool empty = false;
+        if (v < a.vocab) {
+            const int32_t p = first_of(a.keys, a.tokens, (int32_t)v);
+            empty = p == a.tokens || a.keys[p] != (int32_t)v;
+        }
+        constexpr int M = 16 / sizeof(TE);
+        const float zero[M] = {};
+        for (uint64_t todo = __ballot(empty); todo; todo &= todo - 1) {
+            TE *row = static_cast<TE *>(a.dE) + (v0 + __builtin_ctzll(todo)) * a.ldde;
+            for (int c = lane * M; c < a.d; c += kWave * M) {
+                if (a.d - c >= M) store_floats(row + c, zero);
+                else store_floats_part(row + c, a.d - c, zero);
+            }
+        }
+        return;
+    }
+    const int64_t unit = (int64_t)blockIdx.x * kWavesPerBlock + (threadIdx.x >> 6);
+    if (unit >= (int64_t)a.chunks * a.tiles) return;
+    const int64_t c = unit / a.tiles;
+    const int c0 = ((int)(unit % a.tiles) * kWave + lane) * N;
+    const int left = a.d - c0;
+    const int64_t begin = c * a.chunk;
+    const int64_t end = std::min<int64_t>(begin + a.chunk, a.tokens);
+    const TD *src = static_cast<const TD *>(a.dout) + c0;
+    float acc[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] = 0.f;
+    int32_t cur = a.keys[begin];
+    bool began_here = begin == 0 || a.keys[begin - 1] != cur;
+    float *partial = a.partials + c * 2 * a.stride + c0;
+    auto part = [&](float *p) {
+        if (left >= N) store_floats(p, acc);
+        else store_floats_part(p, left, acc);
+    };
+    for (int64_t base = begin; base < end; base += kWave) {
+        const int n = (int)std::min<int64_t>(kWave, end - base);
+        const int32_t my_key = lane < n ? a.keys[base + lane] : a.vocab;
+        const int32_t my_row = lane < n ? a.perm[base + lane] : 0;
+        for (int e0 = 0; e0 < n; e0 += kGradLoads) {
+            float x[kGradLoads][N];
+#pragma unroll
+            for (int u = 0; u < kGradLoads; ++u) {
+                const int e = std::min(e0 + u, n - 1);
+                const int32_t row = __builtin_amdgcn_readlane(my_row, e);
+                const bool wanted = __builtin_amdgcn_readlane(my_key, e) < a.vocab && e0 + u < n;
+                if (wanted && left >= N) {
+                    load_floats(src + row * a.lddo, x[u]);
+                } else if (wanted && left > 0) {
+                    load_floats_part(src + row * a.lddo, left, 0.f, x[u]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) x[u][j] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kGradLoads; ++u) {
+                if (e0 + u >= n) break;
+                const int32_t key = __builtin_amdgcn_readlane(my_key, e0 + u);
+                if (key != cur) {
+                    if (left > 0) {
+                        if (began_here) store_row<TD, TE, N>(a, cur, c0, left, acc);
+                        else part(partial);
+                    }
+                    cur = key;
+                    began_here = true;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] = 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] += x[u][j];
+            }
+            if (cur >= a.vocab) return;  // ids outside the table are the last of the list
+        }
+    }
+    if (left <= 0 || cur >= a.vocab) return;
+    const bool goes_on = end < a.tokens && a.keys[end] == cur;
+    if (!began_here) part(partial);
+    else if (goes_on) part(partial + a.stride);
+    else store_row<TD, TE, N>(a, cur, c0, left, acc);
+}
+
+// Adds up the runs that cross a border between chunks.  A workgroup takes the run that begins in chunk c and goes on behind it, if there
+// is one, and 64 vectors of columns; its wavefronts take equal consecutive shares of the chunks.
+template <typename TE>
+__global__ __launch_bounds__(kBlock) void run_join_kernel(const RunArgs a) {
+    constexpr int N = 4;
+    __shared__ float s_acc[kWavesPerBlock][kWave][N];
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int64_t c = blockIdx.x;
+    const int64_t end = (c + 1) * a.chunk;
+    if (end >= a.tokens) return;
+    const int32_t id = a.keys[end];
+    if (id >= a.vocab || a.keys[end - 1] != id) return;
+    if (a.keys[c * a.chunk] == id && c > 0 && a.keys[c * a.chunk - 1] == id) return;  // began earlier
+    // the chunks behind c that begin with the run: all up to the last whose first id it is
+    int64_t last = c + 1;
+    for (int64_t base = c + 2;; base += kWave) {
+        const int64_t k = base + lane;
+        const bool in = k < a.chunks && a.keys[k * a.chunk] == id;
+        const uint64_t out = ~__ballot(in);
+        last += out ? __builtin_ctzll(out) : kWave;
+        if (out) break;
+    }
+    const int c0 = ((int)blockIdx.y * kWave + lane) * N;
+    const int left = a.d - c0;
+    float acc[N] = {};
+    if (left > 0) {
+        const int64_t n = last - c + 1;  // partial rows: the end of chunk c, then the beginnings of c + 1 ... last
+        const int64_t from = n * wv / kWavesPerBlock, to = n * (wv + 1) / kWavesPerBlock;
+#pragma unroll 8
+        for (int64_t k = from; k < to; ++k) {
+            const float *p = a.partials + ((c + k) * 2 + (k == 0)) * a.stride + c0;  // rows of partials are padded
+            float x[N];
+            load_floats(p, x);
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[j] += x[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) s_acc[wv][lane][j] = acc[j];
+    __syncthreads();
+    if (wv > 0 || left <= 0) return;
+    for (int w = 1; w < kWavesPerBlock; ++w)
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] += s_acc[w][lane][j];
+    store_row<float, TE, N>(a, id, c0, left, acc);
+}
+
+struct GradLayout {
+    uint64_t off_keys[2], off_perm[2], off_counts, off_partials, total;
+    int32_t chunk, chunks;
+    int64_t stride;
+};
+
+// Entries per chunk: as many as leave 4096 wavefronts (16 per CU), counted in tiles of 512 columns, between 8 and 256.
+static GradLayout layout_gradient(int32_t tokens, int32_t d) {
+    GradLayout l{};
+    const int64_t tiles = std::max<int64_t>(1, ((int64_t)d + 511) / 512);
+    l.chunk = 8;
+    while (l.chunk < 256 && (int64_t)tokens * tiles / l.chunk >= 2 * 4096) l.chunk *= 2;
+    l.chunks = (int32_t)(((int64_t)tokens + l.chunk - 1) / l.chunk);
+    l.stride = ((int64_t)d + 63) / 64 * 64;
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        const uint64_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    for (int i = 0; i < 2; ++i) {
+        l.off_keys[i] = take((uint64_t)tokens * 4);
+        l.off_perm[i] = take((uint64_t)tokens * 4);
+    }
+    l.off_counts = take((uint64_t)kSortParts * kBins * 4);
+    l.off_partials = take((uint64_t)l.chunks * 2 * l.stride * 4);
+    l.total = at;
+    return l;
+}
+
+uint64_t gradient_workspace_bytes(int32_t tokens, int32_t d) { return layout_gradient(tokens, d).total; }
+
+scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const int32_t *ids, const void *dout, int32_t dout_type,
+                                int64_t lddo, float scale, int32_t accumulate, void *dE, int32_t de_type, int64_t ldde,
+                                char *workspace, hipStream_t stream) {
+    const GradLayout l = layout_gradient(tokens, d);
+    SortArgs s{};
+    s.tokens = tokens;
+    s.vocab = vocab;
+    s.counts = reinterpret_cast<int32_t *>(workspace + l.off_counts);
+    s.keys_in = ids;
+    const int key_bits = 32 - __builtin_clz((uint32_t)vocab);  // ids go up to vocab itself; vocab > 0
+    const int passes = (key_bits + kDigitBits - 1) / kDigitBits;
+    const int64_t steps = std::max<int64_t>(1, ((int64_t)tokens + kSortStep - 1) / kSortStep);
+    const int64_t part_steps = (steps + kSortParts - 1) / kSortParts;
+    s.part_len = (int32_t)std::min<int64_t>(part_steps * kSortStep, 1 << 30);
+    s.parts = (int32_t)(((int64_t)tokens + s.part_len - 1) / s.part_len);
+    for (int p = 0; p < passes && tokens > 0; ++p) {
+        s.shift = key_bits * p / passes;
+        s.bits = key_bits * (p + 1) / passes - s.shift;
+        s.keys_out = reinterpret_cast<int32_t *>(workspace + l.off_keys[p & 1]);
+        s.perm_out = reinterpret_cast<int32_t *>(workspace + l.off_perm[p & 1]);
+        hipLaunchKernelGGL(sort_count_kernel, dim3((uint32_t)s.parts), dim3(kSortThreads), 0, stream, s);
+        hipLaunchKernelGGL(sort_move_kernel, dim3((uint32_t)s.parts), dim3(kSortThreads), 0, stream, s);
+        s.keys_in = s.keys_out;
+        s.perm_in = s.perm_out;
+    }
+    RunArgs r{};
+    r.keys = s.keys_in;
+    r.perm = s.perm_in;
+    r.dout = dout;
+    r.dE = dE;
+    r.partials = reinterpret_cast<float *>(workspace + l.off_partials);
+    r.lddo = lddo;
+    r.ldde = ldde;
+    r.tokens = tokens;
+    r.vocab = vocab;
+    r.d = d;
+    r.chunk = l.chunk;
+    r.chunks = l.chunks;
+    r.stride = l.stride;
+    r.scale = scale;
+    r.accumulate = accumulate;
+    bool ok = true;
+    ok = with_type(dout_type, [&](auto td) {
+             ok = with_type(de_type, [&](auto te) {
+                 typedef typename decltype(td)::type TD;
+                 typedef typename decltype(te)::type TE;
+                 constexpr int tile = kWave * 16 / (int)sizeof(TD);
+                 r.tiles = (d + tile - 1) / tile;
+                 r.reduce_blocks = ((int64_t)r.chunks * r.tiles + kWavesPerBlock - 1) / kWavesPerBlock;
+                 const int64_t fill = accumulate ? 0 : ((int64_t)vocab + kFillRows * kWavesPerBlock - 1) / (kFillRows * kWavesPerBlock);
+                 if (r.reduce_blocks + fill > 0)
+                     hipLaunchKernelGGL((run_sum_kernel<TD, TE>), dim3((uint32_t)(r.reduce_blocks + fill)), dim3(kBlock), 0, stream, r);
+                 if (r.chunks > 1)
+                     hipLaunchKernelGGL(run_join_kernel<TE>, dim3((uint32_t)(r.chunks - 1), (uint32_t)((d + 255) / 256)), dim3(kBlock), 0, stream, r);
+             });
+         }) && ok;
+    if (!ok) {
+        set_error("embedding gradient: unknown type (%d, %d)", dout_type, de_type);
+        return SCORCH_ERR_INVALID_ARG;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "launch of the embedding gradient");
+    return SCORCH_OK;
+}
+
+}  // namespace scorch

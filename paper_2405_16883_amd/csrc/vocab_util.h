@@ -1,0 +1,64 @@
+// Shared by the kernels in which lists of token ids meet dense rows of 32- or 16-bit floats (embedding.hip, distill.hip, logits.hip).
+#pragma once
+
+#include <math.h>
+
+#include "spmm_internal.h"
+
+namespace scorch {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+// N elements of type T at the alignment of one: gfx950 takes global loads and stores of up to 16 bytes at any address, so rows of odd
+// length or stride need no kernel of their own.
+template <typename T, int N> struct Pack {
+    typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
+// N elements from p as floats.
+template <typename T, int N> __device__ __forceinline__ void load_floats(const T *p, float (&x)[N]) {
+    const typename Pack<T, N>::type v = *reinterpret_cast<const typename Pack<T, N>::type *>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (float)v[i];
+}
+// The first n < N of them; the others are `rest`.
+template <typename T, int N> __device__ __forceinline__ void load_floats_part(const T *p, int n, float rest, float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = i < n ? (float)p[i] : rest;
+}
+// N floats, rounded to the nearest T (ties to even), the only rounding on the way to a 16-bit result.
+template <typename T, int N, bool NT = false> __device__ __forceinline__ void store_floats(T *p, const float (&x)[N]) {
+    typename Pack<T, N>::type v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (T)x[i];
+    auto *q = reinterpret_cast<typename Pack<T, N>::type *>(p);
+    if constexpr (NT) __builtin_nontemporal_store(v, q);
+    else *q = v;
+}
+template <typename T, int N> __device__ __forceinline__ void store_floats_part(T *p, int n, const float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < n) p[i] = (T)x[i];
+}
+
+// 16 bytes of the wider of two types
+template <typename A, typename B> constexpr int kPer16 = 16 / (sizeof(A) > sizeof(B) ? sizeof(A) : sizeof(B));
+
+// A launch has fewer than 2^32 threads in each dimension.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks * threads < (1ll << 32); }
+
+template <typename T> struct type_of {
+    typedef T type;
+};
+// Calls f with a type_of<> of the C type; false if `type` names none.
+template <typename F> bool with_type(int32_t type, F f) {
+    switch (type) {
+        case SCORCH_TYPE_F32: f(type_of<float>()); return true;
+        case SCORCH_TYPE_BF16: f(type_of<bf16>()); return true;
+        case SCORCH_TYPE_F16: f(type_of<f16>()); return true;
+        default: return false;
+    }
+}
+
+}  // namespace scorch
