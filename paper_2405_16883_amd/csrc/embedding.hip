@@ -111,16 +111,15 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / kWave;
 constexpr int kDigitBits = 10;
 constexpr int kBins = 1 << kDigitBits;
-constexpr int kSortRounds = 8;                           // ids per lane and step
-constexpr int kSortStep = kSortThreads * kSortRounds;
-constexpr int kSortParts = 128;                          // workgroups at most
+constexpr int kSortParts = 128;  // workgroups at most
 
 struct SortArgs {
     const int32_t *keys_in, *perm_in;  // perm_in == nullptr: the first pass, the position itself, and keys_in are the caller's ids
     int32_t *keys_out, *perm_out;
-    int32_t *counts;                   // [parts][kBins]
+    int32_t *counts;                   // [parts][bins]
     int32_t tokens, vocab;
-    int32_t parts, part_len;           // a multiple of kSortStep
+    int32_t parts;
+    int64_t part_len;                  // a multiple of what a workgroup takes in one step
     int32_t shift, bits;
 };
 
@@ -132,14 +131,16 @@ __device__ __forceinline__ int32_t sort_key(const SortArgs &a, int64_t i) {
 
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a) {
     __shared__ int32_t s_count[kBins];
+    const int bins = 1 << a.bits;
     s_count[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * a.part_len;
+    const int64_t begin = blockIdx.x * a.part_len;
     const int64_t end = std::min<int64_t>(begin + a.part_len, a.tokens);
+#pragma unroll 4
     for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads)
-        atomicAdd(&s_count[(sort_key(a, i) >> a.shift) & ((1 << a.bits) - 1)], 1);
+        atomicAdd(&s_count[(sort_key(a, i) >> a.shift) & (bins - 1)], 1);
     __syncthreads();
-    a.counts[(int64_t)blockIdx.x * kBins + threadIdx.x] = s_count[threadIdx.x];
+    if ((int)threadIdx.x < bins) a.counts[(int64_t)blockIdx.x * bins + threadIdx.x] = s_count[threadIdx.x];
 }
 
 // The lanes of this wavefront that hold the same digit, of those that take part.
@@ -164,69 +165,163 @@ __device__ __forceinline__ int32_t sort_scan(int32_t x, int32_t *s_wave) {
     if (lane == 63) s_wave[wv] = sum;
     __syncthreads();
     int32_t before = 0;
-    for (int w = 0; w < wv; ++w) before += s_wave[w];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) before += w < wv ? s_wave[w] : 0;
     __syncthreads();
     return before + sum - x;
 }
 
+// ROUNDS: ids per thread and step.
+template <int ROUNDS>
 __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs a) {
-    __shared__ int32_t s_base[kBins];                // where the next id of a digit goes
-    __shared__ int32_t s_count[kSortWaves][kBins];   // of this step, per wavefront; then the wavefront's first place
+    extern __shared__ int32_t s_move[];  // [kSortWaves][bins]: how many of a digit, per wavefront; then where the wavefront's first goes
+    __shared__ int32_t s_base[kBins];    // where the next id of a digit goes
+    __shared__ int32_t s_total[kBins];
     __shared__ int32_t s_wave[kSortWaves];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    int32_t before = 0, total = 0;
-    for (int p = 0; p < a.parts; ++p) {
-        const int32_t c = a.counts[(int64_t)p * kBins + tid];
-        if (p < (int)blockIdx.x) before += c;
-        total += c;
+    const int bins = 1 << a.bits;
+    int32_t *count = s_move + wv * bins;
+    {
+        // where this part's ids go: behind all of lower digits, and those of the same digit in earlier parts
+        s_base[tid] = 0;
+        s_total[tid] = 0;
+        __syncthreads();
+        const int digit = tid & (bins - 1);
+        int32_t before = 0, total = 0;
+#pragma unroll 8
+        for (int p = tid >> a.bits; p < a.parts; p += kSortThreads >> a.bits) {
+            const int32_t c = a.counts[(int64_t)p * bins + digit];
+            before += p < (int)blockIdx.x ? c : 0;
+            total += c;
+        }
+        atomicAdd(&s_base[digit], before);
+        atomicAdd(&s_total[digit], total);
+        __syncthreads();
+        const int32_t lower = sort_scan(tid < bins ? s_total[tid] : 0, s_wave);
+        if (tid < bins) s_base[tid] += lower;
     }
-    s_base[tid] = sort_scan(total, s_wave) + before;
-
-    const int64_t begin = (int64_t)blockIdx.x * a.part_len;
+    const int64_t begin = blockIdx.x * a.part_len;
     const int64_t end = std::min<int64_t>(begin + a.part_len, a.tokens);
-    for (int64_t step = begin; step < end; step += kSortStep) {
-        for (int i = tid; i < kSortWaves * kBins; i += kSortThreads) (&s_count[0][0])[i] = 0;
+    for (int64_t step = begin; step < end; step += kSortThreads * ROUNDS) {
+        int32_t key[ROUNDS], place[ROUNDS];
+        const int64_t mine = step + (int64_t)wv * kWave * ROUNDS + lane;  // a wavefront has consecutive positions
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) key[r] = mine + r * kWave < end ? sort_key(a, mine + r * kWave) : 0;
+        for (int i = tid; i < kSortWaves * bins; i += kSortThreads) s_move[i] = 0;
         __syncthreads();
-        int32_t key[kSortRounds], place[kSortRounds];
-        const int64_t mine = step + (int64_t)wv * kWave * kSortRounds + lane;  // a wavefront has consecutive positions
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r) {
-            const int64_t i = mine + r * kWave;
-            const bool valid = i < end;
-            key[r] = valid ? sort_key(a, i) : 0;
-        }
-#pragma unroll
-        for (int r = 0; r < kSortRounds; ++r) {
+        for (int r = 0; r < ROUNDS; ++r) {
             const bool valid = mine + r * kWave < end;
-            const int digit = key[r] >> a.shift & ((1 << a.bits) - 1);
+            const int digit = key[r] >> a.shift & (bins - 1);
             const uint64_t peers = same_digit(digit, a.bits, valid);
-            place[r] = s_count[wv][digit] + __popcll(peers & ((1ull << lane) - 1));
+            place[r] = count[digit] + __popcll(peers & ((1ull << lane) - 1));
             wave_lds_sync();
-            if (valid && (peers >> lane) == 1) s_count[wv][digit] = place[r] + 1;  // the last of the peers
+            if (valid && (peers >> lane) == 1) count[digit] = place[r] + 1;  // the last of the peers
             wave_lds_sync();
         }
         __syncthreads();
-        {
+        if (tid < bins) {
             int32_t at = s_base[tid];
             for (int w = 0; w < kSortWaves; ++w) {
-                const int32_t c = s_count[w][tid];
-                s_count[w][tid] = at;
+                const int32_t c = s_move[w * bins + tid];
+                s_move[w * bins + tid] = at;
                 at += c;
             }
             s_base[tid] = at;
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r) {
+        for (int r = 0; r < ROUNDS; ++r) {
             const int64_t i = mine + r * kWave;
             if (i < end) {
-                const int digit = key[r] >> a.shift & ((1 << a.bits) - 1);
-                const int32_t to = s_count[wv][digit] + place[r];
+                const int32_t to = count[key[r] >> a.shift & (bins - 1)] + place[r];
                 a.keys_out[to] = key[r];
                 a.perm_out[to] = a.perm_in ? a.perm_in[i] : (int32_t)i;
             }
         }
         __syncthreads();
+    }
+}
+
+// For short lists: one launch, in which a workgroup has a range of ids and a part of the positions.  It reads the whole list, counts the ids of
+// its range and those below it, and so knows where its own go: no workgroup waits for another.
+constexpr int kRankBitsMax = 10;  // ids per range, in bits: 18 counters per id in LDS
+constexpr int kRankRounds = 4;    // ids of its part that a thread holds, at most
+
+struct RankArgs {
+    const int32_t *ids;
+    int32_t *keys_out, *perm_out;
+    int32_t tokens, vocab;
+    int32_t bits;    // of the range
+    int32_t rounds;  // ids per thread of a part
+};
+
+__global__ __launch_bounds__(kSortThreads) void rank_sort_kernel(const RankArgs a) {
+    extern __shared__ int32_t s_rank[];  // [kSortWaves][range]: how many of an id the wavefront has, then where its first one goes
+    __shared__ int32_t s_wave[kSortWaves];
+    __shared__ int32_t s_below;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int range = 1 << a.bits;
+    const int32_t lo = (int32_t)blockIdx.x << a.bits;
+    int32_t *count = s_rank + wv * range;
+    int32_t *s_before = s_rank + kSortWaves * range, *s_rest = s_before + range;  // in the parts before this one, and in the others
+    const int32_t first = (int32_t)blockIdx.y * a.rounds * kSortThreads;          // of this part
+    auto key_of = [&](int32_t id) { return (uint32_t)id >= (uint32_t)a.vocab ? a.vocab : id; };
+    int32_t key[kRankRounds], place[kRankRounds];
+    const int32_t mine = first + wv * kWave * a.rounds + lane;  // a wavefront has consecutive positions
+#pragma unroll
+    for (int r = 0; r < kRankRounds; ++r) {
+        const int32_t i = mine + r * kWave;
+        key[r] = r < a.rounds && i < a.tokens ? key_of(a.ids[i]) : -1;
+    }
+    for (int i = tid; i < (kSortWaves + 2) * range; i += kSortThreads) s_rank[i] = 0;
+    if (tid == 0) s_below = 0;
+    __syncthreads();
+    int32_t below = 0;
+    auto look = [&](int32_t i, int32_t id) {
+        const int32_t k = key_of(id);
+        if (k < lo) ++below;
+        else if (k - lo < range) atomicAdd(i < first ? &s_before[k - lo] : &s_rest[k - lo], 1);
+    };
+    constexpr int W = 4;
+    int32_t i = tid * W;
+#pragma unroll 2
+    for (; i + W <= a.tokens; i += kSortThreads * W) {
+        const typename Pack<int32_t, W>::type id = *reinterpret_cast<const typename Pack<int32_t, W>::type *>(a.ids + i);
+#pragma unroll
+        for (int u = 0; u < W; ++u) look(i + u, id[u]);
+    }
+    for (; i < a.tokens; ++i) look(i, a.ids[i]);  // the last W - 1 at most, of one thread
+    for (int o = 32; o > 0; o /= 2) below += __shfl_xor(below, o);
+    if (lane == 0 && below) atomicAdd(&s_below, below);
+#pragma unroll
+    for (int r = 0; r < kRankRounds; ++r) {
+        const int32_t j = key[r] - lo;
+        const bool here = key[r] >= lo && j < range;  // lo >= 0
+        if (__ballot(here) == 0) continue;
+        const uint64_t peers = same_digit(j, a.bits, here);
+        place[r] = here ? count[j] + __popcll(peers & ((1ull << lane) - 1)) : 0;
+        wave_lds_sync();
+        if (here && (peers >> lane) == 1) count[j] = place[r] + 1;  // the last of the peers
+        wave_lds_sync();
+    }
+    __syncthreads();
+    const int32_t before = tid < range ? s_before[tid] : 0;
+    int32_t at = s_below + sort_scan(tid < range ? before + s_rest[tid] : 0, s_wave) + before;
+    if (tid < range)
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int32_t c = s_rank[w * range + tid];
+            s_rank[w * range + tid] = at;
+            at += c;
+        }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kRankRounds; ++r) {
+        const int32_t j = key[r] - lo;
+        if (key[r] < lo || j >= range) continue;
+        const int32_t to = count[j] + place[r];
+        a.keys_out[to] = key[r];
+        a.perm_out[to] = mine + r * kWave;
     }
 }
 
@@ -457,10 +552,34 @@ static GradLayout layout_gradient(int32_t tokens, int32_t d) {
 
 uint64_t gradient_workspace_bytes(int32_t tokens, int32_t d) { return layout_gradient(tokens, d).total; }
 
-scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const int32_t *ids, const void *dout, int32_t dout_type,
-                                int64_t lddo, float scale, int32_t accumulate, void *dE, int32_t de_type, int64_t ldde,
-                                char *workspace, hipStream_t stream) {
-    const GradLayout l = layout_gradient(tokens, d);
+// The one-launch sort reads the list once per range of ids and part, so it is for as many workgroups as run at once (two per CU) and not too long
+// lists.  Measured, one launch / radix passes: vocabulary 32 000, 256 tokens 4.4 / 11 us, 2048 4.9 / 14, 8192 7.2 / 15, 16 384 9.5 / 16, 32 768
+// 14.5 / 16.6, 65 536 29 / 17; 131 072, 2048 6.8 / 14.5, 8192 10.4 / 18, 16 384 16.1 / 17.3, 32 768 29 / 19; 262 144, 2048 7.7 / 16, 8192 14.9 / 18,
+// 16 384 22 / 19.  Ranges of more ids before parts of more: 32 000 and 8192, 32 ranges x 8 parts 7.2, 126 x 2 8.8, 126 x 8 12.
+constexpr int32_t kRankTokensMax = 32768;
+constexpr int64_t kRankGroups = kCus + 8;  // ranges x parts: the range that holds the key of ids outside the table may be one more
+
+// The token positions in the order of their ids, and of themselves where these are equal; ids outside the table count as vocab.
+static void sort_by_id(int32_t tokens, int32_t vocab, const int32_t *ids, char *workspace, const GradLayout &l, hipStream_t stream,
+                       const int32_t *&keys, const int32_t *&perm) {
+    if (tokens == 0) return;
+    int32_t *keys_out[2], *perm_out[2];
+    for (int i = 0; i < 2; ++i) {
+        keys_out[i] = reinterpret_cast<int32_t *>(workspace + l.off_keys[i]);
+        perm_out[i] = reinterpret_cast<int32_t *>(workspace + l.off_perm[i]);
+    }
+    RankArgs k{ids, keys_out[0], perm_out[0], tokens, vocab, 6, 1};
+    auto ranges = [&] { return ((int64_t)vocab >> k.bits) + 1; };  // of the ids 0 ... vocab
+    auto parts = [&] { return ((int64_t)tokens + k.rounds * kSortThreads - 1) / (k.rounds * kSortThreads); };
+    while (k.bits < kRankBitsMax && ranges() * parts() > kRankGroups) ++k.bits;
+    while (k.rounds < kRankRounds && ranges() * parts() > kRankGroups) k.rounds *= 2;
+    if (tokens <= kRankTokensMax && ranges() * parts() <= 2 * kRankGroups) {
+        hipLaunchKernelGGL(rank_sort_kernel, dim3((uint32_t)ranges(), (uint32_t)parts()), dim3(kSortThreads),
+                           (uint32_t)((kSortWaves + 2) << k.bits) * 4, stream, k);
+        keys = k.keys_out;
+        perm = k.perm_out;
+        return;
+    }
     SortArgs s{};
     s.tokens = tokens;
     s.vocab = vocab;
@@ -468,23 +587,36 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
     s.keys_in = ids;
     const int key_bits = 32 - __builtin_clz((uint32_t)vocab);  // ids go up to vocab itself; vocab > 0
     const int passes = (key_bits + kDigitBits - 1) / kDigitBits;
-    const int64_t steps = std::max<int64_t>(1, ((int64_t)tokens + kSortStep - 1) / kSortStep);
-    const int64_t part_steps = (steps + kSortParts - 1) / kSortParts;
-    s.part_len = (int32_t)std::min<int64_t>(part_steps * kSortStep, 1 << 30);
-    s.parts = (int32_t)(((int64_t)tokens + s.part_len - 1) / s.part_len);
-    for (int p = 0; p < passes && tokens > 0; ++p) {
+    int rounds = 1;
+    while (rounds < 8 && (int64_t)tokens > (int64_t)kSortParts * kSortThreads * rounds) rounds *= 2;
+    const int64_t step = kSortThreads * rounds;
+    const int64_t steps = ((int64_t)tokens + step - 1) / step;
+    s.part_len = (steps + kSortParts - 1) / kSortParts * step;
+    s.parts = (int32_t)((tokens + s.part_len - 1) / s.part_len);
+    const auto move = rounds == 1 ? sort_move_kernel<1> : rounds == 2 ? sort_move_kernel<2> : rounds == 4 ? sort_move_kernel<4> : sort_move_kernel<8>;
+    for (int p = 0; p < passes; ++p) {
         s.shift = key_bits * p / passes;
         s.bits = key_bits * (p + 1) / passes - s.shift;
-        s.keys_out = reinterpret_cast<int32_t *>(workspace + l.off_keys[p & 1]);
-        s.perm_out = reinterpret_cast<int32_t *>(workspace + l.off_perm[p & 1]);
+        s.keys_out = keys_out[p & 1];
+        s.perm_out = perm_out[p & 1];
         hipLaunchKernelGGL(sort_count_kernel, dim3((uint32_t)s.parts), dim3(kSortThreads), 0, stream, s);
-        hipLaunchKernelGGL(sort_move_kernel, dim3((uint32_t)s.parts), dim3(kSortThreads), 0, stream, s);
+        hipLaunchKernelGGL(move, dim3((uint32_t)s.parts), dim3(kSortThreads), (uint32_t)(kSortWaves << s.bits) * 4, stream, s);
         s.keys_in = s.keys_out;
         s.perm_in = s.perm_out;
     }
+    keys = s.keys_in;
+    perm = s.perm_in;
+}
+
+scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const int32_t *ids, const void *dout, int32_t dout_type,
+                                int64_t lddo, float scale, int32_t accumulate, void *dE, int32_t de_type, int64_t ldde,
+                                char *workspace, hipStream_t stream) {
+    const GradLayout l = layout_gradient(tokens, d);
+    const int32_t *keys = nullptr, *perm = nullptr;
+    sort_by_id(tokens, vocab, ids, workspace, l, stream, keys, perm);
     RunArgs r{};
-    r.keys = s.keys_in;
-    r.perm = s.perm_in;
+    r.keys = keys;
+    r.perm = perm;
     r.dout = dout;
     r.dE = dE;
     r.partials = reinterpret_cast<float *>(workspace + l.off_partials);
