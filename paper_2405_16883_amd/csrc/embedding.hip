@@ -12,6 +12,7 @@
 #include "vocab_util.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace scorch {
 
@@ -121,6 +122,7 @@ struct SortArgs {
     int32_t parts;
     int64_t part_len;                  // a multiple of what a workgroup takes in one step
     int32_t shift, bits;
+    int32_t *long_runs;                // set to none
 };
 
 // Ids outside the table become `vocab`: sorted behind all others.
@@ -133,6 +135,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs
     __shared__ int32_t s_count[kBins];
     const int bins = 1 << a.bits;
     s_count[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.long_runs = 0;
     __syncthreads();
     const int64_t begin = blockIdx.x * a.part_len;
     const int64_t end = std::min<int64_t>(begin + a.part_len, a.tokens);
@@ -254,6 +257,7 @@ struct RankArgs {
     int32_t tokens, vocab;
     int32_t bits;    // of the range
     int32_t rounds;  // ids per thread of a part
+    int32_t *long_runs;  // set to none
 };
 
 __global__ __launch_bounds__(kSortThreads) void rank_sort_kernel(const RankArgs a) {
@@ -276,6 +280,7 @@ __global__ __launch_bounds__(kSortThreads) void rank_sort_kernel(const RankArgs 
     }
     for (int i = tid; i < (kSortWaves + 2) * range; i += kSortThreads) s_rank[i] = 0;
     if (tid == 0) s_below = 0;
+    if (blockIdx.x + blockIdx.y == 0 && tid == 0) *a.long_runs = 0;
     __syncthreads();
     int32_t below = 0;
     auto look = [&](int32_t i, int32_t id) {
@@ -296,6 +301,7 @@ __global__ __launch_bounds__(kSortThreads) void rank_sort_kernel(const RankArgs 
     if (lane == 0 && below) atomicAdd(&s_below, below);
 #pragma unroll
     for (int r = 0; r < kRankRounds; ++r) {
+        if (r >= a.rounds) break;
         const int32_t j = key[r] - lo;
         const bool here = key[r] >= lo && j < range;  // lo >= 0
         if (__ballot(here) == 0) continue;
@@ -332,41 +338,29 @@ struct RunArgs {
     const int32_t *keys, *perm;  // sorted by id
     const void *dout;
     void *dE;
-    float *partials;             // [chunks][2][stride]: the run a chunk begins with, if it began before; the run it ends with, if it goes on and began here
+    float *partials;             // [chunks][2][stride]: of the run a chunk begins with, if it began before; of the run that begins in it and goes on
+    int32_t *long_runs;          // how many runs have partial rows, then the chunks that they begin in
     int64_t lddo, ldde;
     int32_t tokens, vocab, d;
     int32_t chunk, chunks;       // entries per chunk
+    int32_t ahead;               // entries behind its chunk that a wavefront takes to finish a run, no more than a chunk has
     int32_t tiles;               // tiles of columns
     int64_t stride;              // of the partial rows
     int64_t reduce_blocks;       // workgroups of the sums; the others store zeros
     float scale;
-    int32_t accumulate;
+    int32_t fill_rows;           // rows of dE per wavefront of those
 };
 
-constexpr int kGradLoads = 8;  // rows of dout in flight per wavefront
-constexpr int kFillRows = 64;  // rows of dE a wavefront looks at for ones without a token
+constexpr int kFillRowsMax = 64;  // rows of dE a wavefront looks at for ones without a token
 
-template <typename TD, typename TE, int N>
-__device__ __forceinline__ void store_row(const RunArgs &a, int32_t id, int c0, int left, const float (&acc)[N]) {
+template <typename TE, int N, bool ADD>
+__device__ __forceinline__ void store_row(const RunArgs &a, int32_t id, int c0, int left, const float (&acc)[N], const typename Pack<TE, N>::type &old) {
     TE *dst = static_cast<TE *>(a.dE) + (int64_t)id * a.ldde + c0;
     float y[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) y[j] = acc[j] * a.scale;
-    if (left >= N) {
-        if (a.accumulate) {
-            float old[N];
-            load_floats(dst, old);
-#pragma unroll
-            for (int j = 0; j < N; ++j) y[j] += old[j];
-        }
-        store_floats(dst, y);
-    } else {
-        if (a.accumulate)
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (j < left) y[j] += (float)dst[j];
-        store_floats_part(dst, left, y);
-    }
+    for (int j = 0; j < N; ++j) y[j] = ADD ? (float)old[j] + acc[j] * a.scale : acc[j] * a.scale;
+    if (left >= N) store_floats(dst, y);
+    else store_floats_part(dst, left, y);
 }
 
 // First place in the sorted list with an id of at least `id`.
@@ -384,144 +378,218 @@ __device__ __forceinline__ int32_t first_of(const int32_t *keys, int32_t n, int3
     return lo;
 }
 
-template <typename TD, typename TE>
+// Rows without a token become zeros: a lane looks one id up, then the wavefront stores row by row.
+template <typename TE> __device__ __forceinline__ void fill_rows(const RunArgs &a, int64_t wave) {
+    const int lane = threadIdx.x & 63;
+    const int64_t v0 = wave * a.fill_rows, v = v0 + lane;
+    bool empty = false;
+    if (lane < a.fill_rows && v < a.vocab) {
+        const int32_t p = first_of(a.keys, a.tokens, (int32_t)v);
+        empty = p == a.tokens || a.keys[p] != (int32_t)v;
+    }
+    constexpr int M = 16 / sizeof(TE);
+    const float zero[M] = {};
+    for (uint64_t todo = __ballot(empty); todo; todo &= todo - 1) {
+        TE *row = static_cast<TE *>(a.dE) + (v0 + __builtin_ctzll(todo)) * a.ldde;
+        for (int c = lane * M; c < a.d; c += kWave * M) {
+            if (a.d - c >= M) store_floats(row + c, zero);
+            else store_floats_part(row + c, a.d - c, zero);
+        }
+    }
+}
+
+// N consecutive elements, the first `left` of them if there are fewer.
+template <typename T, int N> __device__ __forceinline__ typename Pack<T, N>::type load_raw(const T *p, int left) {
+    typename Pack<T, N>::type v = {};
+    if (left >= N) {
+        v = *reinterpret_cast<const typename Pack<T, N>::type *>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) v[i] = p[i];
+    }
+    return v;
+}
+
+// N: columns per lane.  LOADS: rows of dout in flight per wavefront.  ADD: dE holds something already; the row a run ends in is requested with
+// the run's last row of dout, so that no sum waits for it.
+template <typename TD, typename TE, int N, int LOADS, bool ADD>
 __global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
-    constexpr int N = 16 / sizeof(TD);
     const int lane = threadIdx.x & 63;
     if ((int64_t)blockIdx.x >= a.reduce_blocks) {
-        // rows without a token become zeros: a lane looks one id up, then the wavefront stores row by row
-        const int64_t v0 = (((int64_t)blockIdx.x - a.reduce_blocks) * kWavesPerBlock + (threadIdx.x >> 6)) * kFillRows;
-        const int64_t v = v0 + lane;
-        bool empty = false;
-        if (v < a.vocab) {
-            const int32_t p = first_of(a.keys, a.tokens, (int32_t)v);
-            empty = p == a.tokens || a.keys[p] != (int32_t)v;
-        }
-        constexpr int M = 16 / sizeof(TE);
-        const float zero[M] = {};
-        for (uint64_t todo = __ballot(empty); todo; todo &= todo - 1) {
-            TE *row = static_cast<TE *>(a.dE) + (v0 + __builtin_ctzll(todo)) * a.ldde;
-            for (int c = lane * M; c < a.d; c += kWave * M) {
-                if (a.d - c >= M) store_floats(row + c, zero);
-                else store_floats_part(row + c, a.d - c, zero);
-            }
-        }
+        fill_rows<TE>(a, ((int64_t)blockIdx.x - a.reduce_blocks) * kWavesPerBlock + (threadIdx.x >> 6));
         return;
     }
     const int64_t unit = (int64_t)blockIdx.x * kWavesPerBlock + (threadIdx.x >> 6);
     if (unit >= (int64_t)a.chunks * a.tiles) return;
     const int64_t c = unit / a.tiles;
     const int c0 = ((int)(unit % a.tiles) * kWave + lane) * N;
-    const int left = a.d - c0;
+    const int left = a.d - c0;  // none if it is not positive
     const int64_t begin = c * a.chunk;
-    const int64_t end = std::min<int64_t>(begin + a.chunk, a.tokens);
+    const int64_t end = std::min<int64_t>(begin + a.chunk, a.tokens), ahead = std::min<int64_t>(end + a.ahead, a.tokens);
+    auto key_at = [&](int64_t i) { return i >= 0 && i < a.tokens ? a.keys[i] : -1; };
+    const int32_t head = a.keys[begin], tail = a.keys[end - 1];
+    if (head >= a.vocab) return;  // ids outside the table are the last of the list
+    const bool head_earlier = key_at(begin - 1) == head;
+    // A run belongs to the chunk that it begins in, if it does not reach far into the next one.
+    const bool head_taken = head_earlier && key_at(begin - a.chunk - 1) != head && key_at(begin + a.ahead) != head;
+    const bool tail_here = tail < a.vocab && key_at(end) == tail && !(head_earlier && head == tail);  // begins here and goes on
+    const bool tail_whole = tail_here && key_at(ahead) != tail;
+    int64_t stop = end;
+    if (tail_whole)
+        for (int64_t k = end + lane;; k += kWave) {
+            const uint64_t out = ~__ballot(k < ahead && a.keys[k] == tail);
+            stop += out ? __builtin_ctzll(out) : kWave;
+            if (out) break;
+        }
     const TD *src = static_cast<const TD *>(a.dout) + c0;
+    const TE *dst = static_cast<const TE *>(a.dE) + c0;
     float acc[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] = 0.f;
-    int32_t cur = a.keys[begin];
-    bool began_here = begin == 0 || a.keys[begin - 1] != cur;
     float *partial = a.partials + c * 2 * a.stride + c0;
     auto part = [&](float *p) {
         if (left >= N) store_floats(p, acc);
         else store_floats_part(p, left, acc);
     };
-    for (int64_t base = begin; base < end; base += kWave) {
-        const int n = (int)std::min<int64_t>(kWave, end - base);
+    bool began_here = !head_earlier;  // the current run
+    for (int64_t base = begin; base < stop; base += kWave) {
+        const int n = (int)std::min<int64_t>(kWave, stop - base);
         const int32_t my_key = lane < n ? a.keys[base + lane] : a.vocab;
+        const int32_t my_next = lane < n && base + lane + 1 < a.tokens ? a.keys[base + lane + 1] : -1;
         const int32_t my_row = lane < n ? a.perm[base + lane] : 0;
-        for (int e0 = 0; e0 < n; e0 += kGradLoads) {
-            float x[kGradLoads][N];
+        const uint64_t last = __ballot(my_key != my_next);  // of its run
+        int e0 = 0;
+        if (head_taken && !began_here) {
+            const uint64_t others = __ballot(my_key != head);
+            if (others == 0) continue;
+            e0 = __builtin_ctzll(others);
+            began_here = true;
+        }
+        for (; e0 < n; e0 += LOADS) {
+            typename Pack<TD, N>::type x[LOADS];
+            typename Pack<TE, N>::type old[LOADS];
 #pragma unroll
-            for (int u = 0; u < kGradLoads; ++u) {
+            for (int u = 0; u < LOADS; ++u) {
                 const int e = std::min(e0 + u, n - 1);
-                const int32_t row = __builtin_amdgcn_readlane(my_row, e);
-                const bool wanted = __builtin_amdgcn_readlane(my_key, e) < a.vocab && e0 + u < n;
-                if (wanted && left >= N) {
-                    load_floats(src + row * a.lddo, x[u]);
-                } else if (wanted && left > 0) {
-                    load_floats_part(src + row * a.lddo, left, 0.f, x[u]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < N; ++j) x[u][j] = 0.f;
+                x[u] = load_raw<TD, N>(src + __builtin_amdgcn_readlane(my_row, e) * a.lddo, left);
+                if constexpr (ADD) {
+                    const int32_t key = __builtin_amdgcn_readlane(my_key, e);
+                    if (last >> e & 1 && key < a.vocab) old[u] = load_raw<TE, N>(dst + key * a.ldde, left);
                 }
             }
 #pragma unroll
-            for (int u = 0; u < kGradLoads; ++u) {
-                if (e0 + u >= n) break;
-                const int32_t key = __builtin_amdgcn_readlane(my_key, e0 + u);
-                if (key != cur) {
+            for (int u = 0; u < LOADS; ++u) {
+                const int e = e0 + u;
+                if (e >= n) break;
+                const int32_t key = __builtin_amdgcn_readlane(my_key, e);
+                if (key >= a.vocab) return;  // the run before them has been stored
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] += (float)x[u][j];
+                if (last >> e & 1) {
                     if (left > 0) {
-                        if (began_here) store_row<TD, TE, N>(a, cur, c0, left, acc);
+                        if (began_here) store_row<TE, N, ADD>(a, key, c0, left, acc, old[u]);
                         else part(partial);
                     }
-                    cur = key;
                     began_here = true;
 #pragma unroll
                     for (int j = 0; j < N; ++j) acc[j] = 0.f;
                 }
-#pragma unroll
-                for (int j = 0; j < N; ++j) acc[j] += x[u][j];
             }
-            if (cur >= a.vocab) return;  // ids outside the table are the last of the list
         }
     }
-    if (left <= 0 || cur >= a.vocab) return;
-    const bool goes_on = end < a.tokens && a.keys[end] == cur;
-    if (!began_here) part(partial);
-    else if (goes_on) part(partial + a.stride);
-    else store_row<TD, TE, N>(a, cur, c0, left, acc);
+    // a run that goes on
+    if (key_at(end) != tail || tail_whole || (head_taken && head == tail)) return;
+    if (left > 0) part(tail_here ? partial + a.stride : partial);
+    if (tail_here && unit % a.tiles == 0 && lane == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1)] = (int32_t)c;
 }
 
-// Adds up the runs that cross a border between chunks.  A workgroup takes the run that begins in chunk c and goes on behind it, if there
-// is one, and 64 vectors of columns; its wavefronts take equal consecutive shares of the chunks.
-template <typename TE>
-__global__ __launch_bounds__(kBlock) void run_join_kernel(const RunArgs a) {
+// Adds up the runs that have partial rows, which are listed in any order.  A wavefront takes a run and 64 vectors of columns; if it has
+// more than a few partial rows, the wavefronts of the workgroup share it, in equal consecutive shares.
+constexpr int kJoinThreads = 1024;
+constexpr int kJoinWaves = kJoinThreads / kWave;
+constexpr int kJoinLoads = 8;   // in flight
+constexpr int kJoinShort = 32;  // partial rows that are one wavefront's
+
+template <typename TE, bool ADD>
+__global__ __launch_bounds__(kJoinThreads) void run_join_kernel(const RunArgs a) {
     constexpr int N = 4;
-    __shared__ float s_acc[kWavesPerBlock][kWave][N];
+    __shared__ float s_acc[kJoinWaves][kWave][N];
+    __shared__ int64_t s_rows[kJoinWaves];
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int64_t c = blockIdx.x;
-    const int64_t end = (c + 1) * a.chunk;
-    if (end >= a.tokens) return;
-    const int32_t id = a.keys[end];
-    if (id >= a.vocab || a.keys[end - 1] != id) return;
-    if (a.keys[c * a.chunk] == id && c > 0 && a.keys[c * a.chunk - 1] == id) return;  // began earlier
-    // the chunks behind c that begin with the run: all up to the last whose first id it is
-    int64_t last = c + 1;
-    for (int64_t base = c + 2;; base += kWave) {
-        const int64_t k = base + lane;
-        const bool in = k < a.chunks && a.keys[k * a.chunk] == id;
-        const uint64_t out = ~__ballot(in);
-        last += out ? __builtin_ctzll(out) : kWave;
-        if (out) break;
-    }
     const int c0 = ((int)blockIdx.y * kWave + lane) * N;
     const int left = a.d - c0;
-    float acc[N] = {};
-    if (left > 0) {
-        const int64_t n = last - c + 1;  // partial rows: the end of chunk c, then the beginnings of c + 1 ... last
-        const int64_t from = n * wv / kWavesPerBlock, to = n * (wv + 1) / kWavesPerBlock;
-#pragma unroll 8
-        for (int64_t k = from; k < to; ++k) {
-            const float *p = a.partials + ((c + k) * 2 + (k == 0)) * a.stride + c0;  // rows of partials are padded
-            float x[N];
-            load_floats(p, x);
+    // partial rows k in [from, to) of the run that begins in chunk c: the end of c, then the beginnings of c + 1, ...
+    auto add = [&](int64_t c, int64_t from, int64_t to, float (&acc)[N]) {
+        if (left <= 0) return;
+        for (int64_t k0 = from; k0 < to; k0 += kJoinLoads) {
+            float x[kJoinLoads][N];
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] += x[j];
+            for (int u = 0; u < kJoinLoads; ++u) {
+                const int64_t k = std::min(k0 + u, to - 1);
+                load_floats(a.partials + ((c + k) * 2 + (k == 0)) * a.stride + c0, x[u]);  // rows of partials are padded
+            }
+#pragma unroll
+            for (int u = 0; u < kJoinLoads; ++u)
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] += k0 + u < to ? x[u][j] : 0.f;
         }
+    };
+    auto finish = [&](int32_t id, float (&acc)[N]) {
+        if (left <= 0) return;
+        typename Pack<TE, N>::type old = {};
+        if constexpr (ADD) old = load_raw<TE, N>(static_cast<const TE *>(a.dE) + id * a.ldde + c0, left);
+        store_row<TE, N, ADD>(a, id, c0, left, acc, old);
+    };
+    const int32_t n_runs = a.long_runs[0];
+    // neighbours in the list, often long runs next to each other, go to different workgroups
+    for (int32_t first = (int32_t)blockIdx.x; first < n_runs; first += (int32_t)gridDim.x * kJoinWaves) {
+        int64_t rows = 0;
+        const int64_t mine = first + (int64_t)wv * gridDim.x;
+        if (mine < n_runs) {
+            const int64_t c = a.long_runs[1 + mine];
+            const int32_t id = a.keys[(c + 1) * a.chunk];
+            // the chunks behind c that begin with the run: all up to the last whose first id it is
+            for (rows = 2;; rows += kWave) {
+                const int64_t k = c + rows + lane;
+                const uint64_t out = ~__ballot(k < a.chunks && a.keys[k * a.chunk] == id);
+                if (out) {
+                    rows += __builtin_ctzll(out);
+                    break;
+                }
+            }
+            if (rows <= kJoinShort) {
+                float acc[N] = {};
+                add(c, 0, rows, acc);
+                finish(id, acc);
+                rows = 0;
+            }
+        }
+        if (lane == 0) s_rows[wv] = rows;
+        __syncthreads();
+        for (int w = 0; w < kJoinWaves; ++w) {
+            const int64_t n = s_rows[w];
+            if (n == 0) continue;
+            const int64_t c = a.long_runs[1 + first + (int64_t)w * gridDim.x];
+            float acc[N] = {};
+            add(c, n * wv / kJoinWaves, n * (wv + 1) / kJoinWaves, acc);
+#pragma unroll
+            for (int j = 0; j < N; ++j) s_acc[wv][lane][j] = acc[j];
+            __syncthreads();
+            if (wv == 0) {
+                for (int o = 1; o < kJoinWaves; ++o)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] += s_acc[o][lane][j];
+                finish(a.keys[(c + 1) * a.chunk], acc);
+            }
+            __syncthreads();
+        }
+        __syncthreads();
     }
-#pragma unroll
-    for (int j = 0; j < N; ++j) s_acc[wv][lane][j] = acc[j];
-    __syncthreads();
-    if (wv > 0 || left <= 0) return;
-    for (int w = 1; w < kWavesPerBlock; ++w)
-#pragma unroll
-        for (int j = 0; j < N; ++j) acc[j] += s_acc[w][lane][j];
-    store_row<float, TE, N>(a, id, c0, left, acc);
 }
 
 struct GradLayout {
-    uint64_t off_keys[2], off_perm[2], off_counts, off_partials, total;
+    uint64_t off_keys[2], off_perm[2], off_counts, off_long, off_partials, total;
     int32_t chunk, chunks;
     int64_t stride;
 };
@@ -545,6 +613,7 @@ static GradLayout layout_gradient(int32_t tokens, int32_t d) {
         l.off_perm[i] = take((uint64_t)tokens * 4);
     }
     l.off_counts = take((uint64_t)kSortParts * kBins * 4);
+    l.off_long = take(((uint64_t)l.chunks + 1) * 4);
     l.off_partials = take((uint64_t)l.chunks * 2 * l.stride * 4);
     l.total = at;
     return l;
@@ -568,7 +637,8 @@ static void sort_by_id(int32_t tokens, int32_t vocab, const int32_t *ids, char *
         keys_out[i] = reinterpret_cast<int32_t *>(workspace + l.off_keys[i]);
         perm_out[i] = reinterpret_cast<int32_t *>(workspace + l.off_perm[i]);
     }
-    RankArgs k{ids, keys_out[0], perm_out[0], tokens, vocab, 6, 1};
+    int32_t *long_runs = reinterpret_cast<int32_t *>(workspace + l.off_long);
+    RankArgs k{ids, keys_out[0], perm_out[0], tokens, vocab, 6, 1, long_runs};
     auto ranges = [&] { return ((int64_t)vocab >> k.bits) + 1; };  // of the ids 0 ... vocab
     auto parts = [&] { return ((int64_t)tokens + k.rounds * kSortThreads - 1) / (k.rounds * kSortThreads); };
     while (k.bits < kRankBitsMax && ranges() * parts() > kRankGroups) ++k.bits;
@@ -584,6 +654,7 @@ static void sort_by_id(int32_t tokens, int32_t vocab, const int32_t *ids, char *
     s.tokens = tokens;
     s.vocab = vocab;
     s.counts = reinterpret_cast<int32_t *>(workspace + l.off_counts);
+    s.long_runs = long_runs;
     s.keys_in = ids;
     const int key_bits = 32 - __builtin_clz((uint32_t)vocab);  // ids go up to vocab itself; vocab > 0
     const int passes = (key_bits + kDigitBits - 1) / kDigitBits;
@@ -620,6 +691,7 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
     r.dout = dout;
     r.dE = dE;
     r.partials = reinterpret_cast<float *>(workspace + l.off_partials);
+    r.long_runs = reinterpret_cast<int32_t *>(workspace + l.off_long);
     r.lddo = lddo;
     r.ldde = ldde;
     r.tokens = tokens;
@@ -627,22 +699,31 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
     r.d = d;
     r.chunk = l.chunk;
     r.chunks = l.chunks;
+    r.ahead = std::max(8, l.chunk / 4);
     r.stride = l.stride;
     r.scale = scale;
-    r.accumulate = accumulate;
     bool ok = true;
     ok = with_type(dout_type, [&](auto td) {
              ok = with_type(de_type, [&](auto te) {
                  typedef typename decltype(td)::type TD;
                  typedef typename decltype(te)::type TE;
-                 constexpr int tile = kWave * 16 / (int)sizeof(TD);
-                 r.tiles = (d + tile - 1) / tile;
+                 constexpr int N = 16 / sizeof(TD);
+                 r.tiles = (d + kWave * N - 1) / (kWave * N);
                  r.reduce_blocks = ((int64_t)r.chunks * r.tiles + kWavesPerBlock - 1) / kWavesPerBlock;
-                 const int64_t fill = accumulate ? 0 : ((int64_t)vocab + kFillRows * kWavesPerBlock - 1) / (kFillRows * kWavesPerBlock);
-                 if (r.reduce_blocks + fill > 0)
-                     hipLaunchKernelGGL((run_sum_kernel<TD, TE>), dim3((uint32_t)(r.reduce_blocks + fill)), dim3(kBlock), 0, stream, r);
-                 if (r.chunks > 1)
-                     hipLaunchKernelGGL(run_join_kernel<TE>, dim3((uint32_t)(r.chunks - 1), (uint32_t)((d + 255) / 256)), dim3(kBlock), 0, stream, r);
+                 int64_t fill = 0;
+                 if (!accumulate) {  // some 8192 wavefronts
+                     r.fill_rows = 4;
+                     while (r.fill_rows < kFillRowsMax && vocab / r.fill_rows > 8192) r.fill_rows *= 2;
+                     fill = ((int64_t)vocab + r.fill_rows * kWavesPerBlock - 1) / (r.fill_rows * kWavesPerBlock);
+                 }
+                 const dim3 sums((uint32_t)(r.reduce_blocks + fill)), joins((uint32_t)std::max(1, std::min((r.chunks + kJoinWaves - 1) / kJoinWaves, 2 * kCus / ((d + 255) / 256))), (uint32_t)((d + 255) / 256));
+                 auto launch = [&](auto add) {
+                     constexpr bool ADD = decltype(add)::value;
+                     if (sums.x > 0) hipLaunchKernelGGL((run_sum_kernel<TD, TE, N, ADD ? 4 : 8, ADD>), sums, dim3(kBlock), 0, stream, r);
+                     if (r.chunks > 2) hipLaunchKernelGGL((run_join_kernel<TE, ADD>), joins, dim3(kJoinThreads), 0, stream, r);
+                 };
+                 if (accumulate) launch(std::true_type());
+                 else launch(std::false_type());
              });
          }) && ok;
     if (!ok) {

@@ -222,8 +222,8 @@ scorch_status_t launch_logits(int32_t rows, int32_t vocab, const void *in, int32
                      hipLaunchKernelGGL((logits_kernel<TI, TO, H, B>), dim3((uint32_t)grid), dim3(kLogitsThreads),
                                         (LogitsLds<H, B>::bytes(a.tile)), stream, a);
                  };
-                 typedef std::integral_constant<bool, true> yes;
-                 typedef std::integral_constant<bool, false> no;
+                 typedef std::true_type yes;
+                 typedef std::false_type no;
                  if (rules.history_rowptr && rules.bias_rowptr) launch(yes(), yes());
                  else if (rules.history_rowptr) launch(yes(), no());
                  else if (rules.bias_rowptr) launch(no(), yes());
