@@ -16,8 +16,6 @@
 
 namespace scorch {
 
-constexpr int kDistillThreads = 1024;
-constexpr int kDistillWaves = kDistillThreads / kWave;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 enum { kDistillLoss = 1, kDistillGradient = 2 };  // what a kernel computes; both: 3
@@ -30,7 +28,8 @@ struct DistillArgs {
     float *loss, *stats;
     int64_t ldz, lddz;
     int32_t rows, vocab;
-    float x;  // 1 / temperature
+    float x;       // 1 / temperature
+    int32_t part;  // the gradient alone: columns per workgroup, a power of two
 };
 
 struct Max {
@@ -40,101 +39,202 @@ struct Sum {
     __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };
 
-template <typename OP> __device__ __forceinline__ float wave_all(float v, OP op) {
-    v = op(v, lane_xor<1>(v));
-    v = op(v, lane_xor<2>(v));
-    v = op(v, lane_xor<4>(v));
-    v = op(v, lane_xor<8>(v));
-    v = op(v, lane_xor<16>(v));
-    return op(v, lane_xor<32>(v));
+// Over all lanes whose numbers differ in bits below LANES only
+template <int LANES, typename OP> __device__ __forceinline__ float lanes_all(float v, OP op) {
+    if constexpr (LANES > 1) v = op(v, lane_xor<1>(v));
+    if constexpr (LANES > 2) v = op(v, lane_xor<2>(v));
+    if constexpr (LANES > 4) v = op(v, lane_xor<4>(v));
+    if constexpr (LANES > 8) v = op(v, lane_xor<8>(v));
+    if constexpr (LANES > 16) v = op(v, lane_xor<16>(v));
+    if constexpr (LANES > 32) v = op(v, lane_xor<32>(v));
+    return v;
 }
-// Over all threads of the workgroup, two values at a time; s: LDS of two values per wavefront, free before and after.
-template <typename OP> __device__ __forceinline__ void block_all(float &u, float &v, OP op, float (&s)[2][kDistillWaves]) {
-    u = wave_all(u, op);
-    v = wave_all(v, op);
-    const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (lane == 0) {
-        s[0][wv] = u;
-        s[1][wv] = v;
-    }
-    __syncthreads();
-    u = s[0][0];
-    v = s[1][0];
-    for (int w = 1; w < kDistillWaves; ++w) {
-        u = op(u, s[0][w]);
-        v = op(v, s[1][w]);
-    }
-    __syncthreads();
-}
-
-template <typename T, int WHAT>
-__global__ __launch_bounds__(kDistillThreads) void distill_kernel(const DistillArgs a) {
-    constexpr int N = 16 / sizeof(T);
-    constexpr bool kLoss = WHAT & kDistillLoss, kGradient = WHAT & kDistillGradient;
-    extern __shared__ uint32_t s_marks[];  // gradient: a bit per column with an entry, then one per column with several
-    __shared__ float s_red[2][kDistillWaves];
-    const int tid = threadIdx.x;
-    const int64_t row = blockIdx.x;
-    const T *z = static_cast<const T *>(a.Z) + row * a.ldz;
-    const int32_t p0 = a.rowptr[row], p1 = a.rowptr[row + 1];
-    const float k = a.x * kLog2e;
-    const int words = (a.vocab + 31) / 32;
-    uint32_t *s_twice = s_marks + words;
-    auto stored = [&](int32_t p, int32_t &col, float &t) {
-        col = a.colidx[p];
-        t = a.vals[p];
-        return (uint32_t)col < (uint32_t)a.vocab && t != -INFINITY;
-    };
-
-    if constexpr (kGradient) {
-        for (int i = tid; i < 2 * words; i += kDistillThreads) s_marks[i] = 0;
+// Over all threads of the workgroup, two values at a time; s: LDS of two values per wavefront that nothing else uses.
+template <int WAVES, typename OP> __device__ __forceinline__ void block_all(float &u, float &v, OP op, float (&s)[2][WAVES]) {
+    u = lanes_all<kWave>(u, op);
+    v = lanes_all<kWave>(v, op);
+    if constexpr (WAVES > 1) {
+        const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        if (lane == 0) {
+            s[0][wv] = u;
+            s[1][wv] = v;
+        }
         __syncthreads();
+        u = lanes_all<WAVES>(s[0][lane & (WAVES - 1)], op);
+        v = lanes_all<WAVES>(s[1][lane & (WAVES - 1)], op);
     }
-    // largest logits, of the student's row and of the stored entries; the sums go along with a maximum of each thread's own
-    float top = -INFINITY, sum = 0.f, t_top = -INFINITY, t_any = 0.f;
-    if constexpr (kLoss) {
-        for (int j = tid * N; j < a.vocab; j += kDistillThreads * N) {
-            float y[N];
-            if (a.vocab - j >= N) load_floats(z + j, y);
-            else load_floats_part(z + j, a.vocab - j, -INFINITY, y);
+}
+
+// A row of logits in vectors at multiples of 16 bytes, of which every thread keeps the first HELD in registers; what is behind them is read again
+// by every pass.  The columns before the first vector and behind the last, fewer than threads, are one each of the first threads.  (Vectors from the
+// row's first column on, wherever that is: 131 071 columns of 16 bits 18 % slower.)
+template <typename T, int THREADS, int HELD> struct LogitRow {
+    static constexpr int N = 16 / sizeof(T);
+    static constexpr int kStep = THREADS * N;
+    const T *z;        // at the first vector
+    int32_t whole;     // columns in vectors
+    int32_t skip;      // columns before them
+    int32_t extra;     // this thread's column outside them, counted from the first vector
+    bool has_extra;
+    float extra_z;
+    raw16 held[HELD > 0 ? HELD : 1];
+
+    __device__ __forceinline__ LogitRow(const T *row, int32_t vocab) {
+        skip = std::min(vocab, (int32_t)(-reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)));
+        z = row + skip;
+        whole = (vocab - skip) / N * N;
+        has_extra = whole + (int)threadIdx.x < vocab;
+        extra = (int)threadIdx.x < skip ? (int)threadIdx.x - skip : whole + (int)threadIdx.x - skip;
+        extra_z = has_extra ? (float)z[extra] : -INFINITY;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) held[u] = holds(u) ? load_raw16(mine(z, u)) : nothing();
+    }
+    // Where this thread's vector u is in a row: the row's address is the same for all lanes, the offset takes one register for all u.
+    template <typename P> static __device__ __forceinline__ P *mine(P *row, int u) {
+        return reinterpret_cast<P *>(reinterpret_cast<uintptr_t>(row + u * kStep) + threadIdx.x * 16u);
+    }
+    // -infinity throughout: without a share
+    static __device__ __forceinline__ raw16 nothing() {
+        const uint32_t w = sizeof(T) == 4 ? 0xff800000u : std::is_same_v<T, bf16> ? 0xff80ff80u : 0xfc00fc00u;
+        return raw16{w, w, w, w};
+    }
+    // Between passes: without it, the compiler keeps the floats of the held vectors from pass to pass, in twice the registers.
+    __device__ __forceinline__ void forget_floats() {
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) asm volatile("" : "+v"(held[u]));
+    }
+    __device__ __forceinline__ bool holds(int u) const { return u * kStep + (int)threadIdx.x * N < whole; }
+    // f(first column counted from the first vector, where that is in `to`, vector) for all vectors of this thread
+    template <typename F> __device__ __forceinline__ void each(T *to, F f) const {
+        const int32_t j0 = (int)threadIdx.x * N;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            if (holds(u)) f(u * kStep + j0, mine(to, u), held[u]);
+            __builtin_amdgcn_sched_barrier(0);  // one after the other: what is not held has to fit into few registers
+        }
+        for (int32_t j = HELD * kStep + j0; j < whole; j += kStep) f(j, to + j, load_raw16(z + j));
+    }
+    // The largest logit of this thread among those that are not held, and the sum of exp2((z - largest) k) over them; not a number if there is
+    // one that is not.
+    __device__ __forceinline__ void sum_with_max(float k, float &top, float &sum) const {
+        constexpr int U = HELD > 0 ? 8 / N : 4;  // vectors in flight
+        top = extra_z == extra_z ? extra_z : -INFINITY;
+        sum = extra_z == extra_z ? (extra_z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((extra_z - extra_z) * k)) : NAN;
+        for (int32_t j0 = HELD * kStep + (int)threadIdx.x * N; j0 < whole; j0 += U * kStep) {
+            raw16 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = j0 + (int64_t)u * kStep < whole ? load_raw16(z + j0 + u * kStep) : nothing();
             float m = top;
 #pragma unroll
-            for (int i = 0; i < N; ++i) m = fmaxf(m, y[i]);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i) m = fmaxf(m, element<T>(v[u], i));
             if (m == -INFINITY) {
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (y[i] != y[i]) sum = NAN;
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (element<T>(v[u], i) != element<T>(v[u], i)) sum = NAN;
                 continue;
             }
             sum *= __builtin_amdgcn_exp2f((top - m) * k);
             top = m;
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum += __builtin_amdgcn_exp2f((y[i] - m) * k);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum += __builtin_amdgcn_exp2f((element<T>(v[u], i) - m) * k);
         }
     }
-    for (int32_t p = p0 + tid; p < p1; p += kDistillThreads) {
-        int32_t col;
-        float t;
-        if (!stored(p, col, t)) continue;
-        t_top = fmaxf(t_top, t);
-        t_any = 1.f;
+};
+
+// Words for a bit per column, from bit 32 less what stands before the first vector on.
+__host__ __device__ constexpr int mark_words(int32_t cols) { return (cols + 31) / 32 + 1; }
+
+// A workgroup has a row (the gradient alone: `part` columns of one, blockIdx.y-th).
+template <typename T, int WHAT, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(const DistillArgs a) {
+    typedef LogitRow<T, THREADS, HELD> Row;
+    constexpr int N = Row::N;
+    constexpr int kWaves = THREADS / kWave;
+    constexpr bool kLoss = WHAT & kDistillLoss, kGradient = WHAT & kDistillGradient;
+    extern __shared__ uint32_t s_marks[];  // gradient: a bit per column with an entry, then one per column with several
+    __shared__ float s_red[3][2][kWaves];
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const int32_t lo = kLoss ? 0 : (int32_t)blockIdx.y * a.part;
+    const int32_t cols = kLoss ? a.vocab : std::min(a.part, a.vocab - lo);
+    Row z(static_cast<const T *>(a.Z) + row * a.ldz + lo, cols);
+    const int32_t p0 = a.rowptr[row], p1 = a.rowptr[row + 1];
+    const float k = a.x * kLog2e;
+    const int words = mark_words(cols);
+    uint32_t *s_twice = s_marks + words;
+    auto bit_of = [&](int32_t col) { return (uint32_t)(col - z.skip + 32); };  // a vector's bits are in one word
+    // An entry that counts as stored; col < 0 or >= cols: a column of another part.
+    struct Entry {
+        int32_t p, col;
+        float t, z;
+        bool stored;
+    };
+    auto read = [&](int32_t p) {
+        Entry e{p, 0, 0.f, 0.f, p < p1};
+        if (!e.stored) return e;
+        e.col = a.colidx[p];
+        e.t = a.vals[p];
+        e.stored = (uint32_t)e.col < (uint32_t)a.vocab && e.t != -INFINITY;
+        e.col -= lo;
+        if (e.stored && (kLoss || (uint32_t)e.col < (uint32_t)cols)) e.z = (float)z.z[e.col - z.skip];
+        return e;
+    };
+    const Entry own = read(p0 + tid);  // most rows have no more than one per thread: read once
+    auto entries = [&](auto f) {
+        if (own.stored) f(own);
+        for (int32_t p = p0 + tid; p1 - p > THREADS;) {
+            p += THREADS;
+            const Entry e = read(p);
+            if (e.stored) f(e);
+        }
+    };
+    if constexpr (kGradient) {
+        for (int i = tid; i < 2 * words; i += THREADS) s_marks[i] = 0;
+        __syncthreads();
+    }
+    float t_top = -INFINITY;
+    entries([&](const Entry &e) {
+        t_top = fmaxf(t_top, e.t);
         if constexpr (kGradient) {
-            const uint32_t bit = 1u << (col & 31);
-            if (atomicOr(&s_marks[col >> 5], bit) & bit) atomicOr(&s_twice[col >> 5], bit);
+            if ((uint32_t)e.col >= (uint32_t)cols) return;
+            const uint32_t b = bit_of(e.col), bit = 1u << (b & 31);
+            if (atomicOr(&s_marks[b >> 5], bit) & bit) atomicOr(&s_twice[b >> 5], bit);
+        }
+    });
+    // largest logits, of the student's row and of the stored entries, then the sums
+    float top = -INFINITY, sum = 0.f, z_top = 0.f;
+    if constexpr (kLoss) {
+        z.sum_with_max(k, top, sum);
+        z_top = top;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u)
+            if (z.holds(u))
+#pragma unroll
+                for (int i = 0; i < N; ++i) z_top = fmaxf(z_top, element<T>(z.held[u], i));
+    }
+    z.forget_floats();
+    block_all(z_top, t_top, Max(), s_red[0]);
+    if constexpr (kLoss) {
+        sum = top == -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((top - z_top) * k);
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            if (z.holds(u))
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum += __builtin_amdgcn_exp2f((element<T>(z.held[u], i) - z_top) * k);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
-    float z_top = top;
-    block_all(z_top, t_top, Max(), s_red);
-    if constexpr (kLoss) sum = top == -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((top - z_top) * k);
+    z.forget_floats();
     float t_sum = 0.f;
-    for (int32_t p = p0 + tid; p < p1; p += kDistillThreads) {
-        int32_t col;
-        float t;
-        if (stored(p, col, t)) t_sum += __builtin_amdgcn_exp2f((t - t_top) * k);
-    }
-    block_all(sum, t_sum, Sum(), s_red);
-    float divergence = 0.f;
-    block_all(t_any, divergence, Max(), s_red);
+    entries([&](const Entry &e) { t_sum += __builtin_amdgcn_exp2f((e.t - t_top) * k); });
+    block_all(sum, t_sum, Sum(), s_red[1]);
+    const bool none = t_sum == 0.f;  // otherwise the largest entry's share is 1, or something is not a number
     if constexpr (!kLoss) {
         z_top = a.stats[2 * row];
         sum = a.stats[2 * row + 1];
@@ -142,86 +242,105 @@ __global__ __launch_bounds__(kDistillThreads) void distill_kernel(const DistillA
     const float t_scale = 1.f / t_sum;
     if constexpr (kLoss) {
         const float log_sums = logf(t_sum) - logf(sum);
-        for (int32_t p = p0 + tid; p < p1; p += kDistillThreads) {
-            int32_t col;
-            float t;
-            if (!stored(p, col, t)) continue;
-            const float prob = __builtin_amdgcn_exp2f((t - t_top) * k) * t_scale;
-            const float zk = (float)z[col];
-            if (prob != 0.f) divergence += prob * (a.x * (t - t_top) - a.x * (zk - z_top) - log_sums);
-        }
-        float unused = 0.f;
-        block_all(divergence, unused, Sum(), s_red);
+        float divergence = 0.f, unused = 0.f;
+        entries([&](const Entry &e) {
+            const float prob = __builtin_amdgcn_exp2f((e.t - t_top) * k) * t_scale;
+            if (prob != 0.f) divergence += prob * (a.x * (e.t - t_top) - a.x * (e.z - z_top) - log_sums);
+        });
+        block_all(divergence, unused, Sum(), s_red[2]);
         if (tid == 0) {
             a.loss[row] = divergence;
-            if (a.stats) {
+            if (!kGradient) {
                 a.stats[2 * row] = z_top;
                 a.stats[2 * row + 1] = sum;
             }
         }
     }
     if constexpr (kGradient) {
-        T *dz = static_cast<T *>(a.dZ) + row * a.lddz;
+        T *dz = static_cast<T *>(a.dZ) + row * a.lddz + lo;
         const float c = (a.dloss ? a.dloss[row] : 1.f) * a.x;
-        const bool none = t_any == 0.f;
-        const float q_scale = 1.f / sum;
-        for (int32_t p = p0 + tid; p < p1; p += kDistillThreads) {
-            int32_t col;
-            float t;
-            if (!stored(p, col, t)) continue;
-            float prob = __builtin_amdgcn_exp2f((t - t_top) * k) * t_scale;
-            if (s_twice[col >> 5] >> (col & 31) & 1) {
-                // the column's first entry adds the others up and is the only one to read and write there
+        const float q_scale = 1.f / sum, cq = c * q_scale;
+        entries([&](const Entry &e) {
+            if ((uint32_t)e.col >= (uint32_t)cols) return;
+            float prob = __builtin_amdgcn_exp2f((e.t - t_top) * k) * t_scale;
+            if (s_twice[bit_of(e.col) >> 5] >> (bit_of(e.col) & 31) & 1) {
+                // the column's first entry adds the others up and is the only one to write there
                 bool first = true;
-                for (int32_t o = p0; o < p && first; ++o) {
-                    int32_t other;
-                    first = !(stored(o, other, t) && other == col);
-                }
-                if (!first) continue;
-                for (int32_t o = p + 1; o < p1; ++o) {
-                    int32_t other;
-                    if (stored(o, other, t) && other == col) prob += __builtin_amdgcn_exp2f((t - t_top) * k) * t_scale;
-                }
+                for (int32_t o = p0; o < e.p && first; ++o) first = !(a.colidx[o] - lo == e.col && a.vals[o] != -INFINITY);
+                if (!first) return;
+                for (int32_t o = e.p + 1; o < p1; ++o)
+                    if (a.colidx[o] - lo == e.col && a.vals[o] != -INFINITY) prob += __builtin_amdgcn_exp2f((a.vals[o] - t_top) * k) * t_scale;
             }
-            dz[col] = (T)(c * (__builtin_amdgcn_exp2f(((float)z[col] - z_top) * k) * q_scale - prob));
-        }
-        for (int j = tid * N; j < a.vocab; j += kDistillThreads * N) {
-            const int n = std::min(N, a.vocab - j);
-            const uint32_t marks = s_marks[j >> 5] >> (j & 31) & ((1u << N) - 1);
+            dz[e.col] = (T)(c * (__builtin_amdgcn_exp2f((e.z - z_top) * k) * q_scale - prob));
+        });
+        // Streaming stores: written once, and the memory-side cache is left to the logits that are read again
+        z.each(dz + z.skip, [&](int32_t j, T *to, const raw16 &v) {
+            const uint32_t marks = s_marks[(j >> 5) + 1] >> (j & 31) & ((1u << N) - 1);
             float y[N];
-            if (n == N) load_floats(z + j, y);
-            else load_floats_part(z + j, n, 0.f, y);
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = none ? 0.f : c * (__builtin_amdgcn_exp2f((y[i] - z_top) * k) * q_scale);
-            if (n == N && marks == 0) {
-                store_floats(dz + j, y);
+            for (int i = 0; i < N; ++i) y[i] = none ? 0.f : cq * __builtin_amdgcn_exp2f((element<T>(v, i) - z_top) * k);
+            if (marks == 0) {
+                store_floats<T, N, true>(to, y);
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    if (i < n && !(marks >> i & 1)) dz[j + i] = (T)y[i];
+                    if (!(marks >> i & 1)) to[i] = (T)y[i];
             }
-        }
+        });
+        const uint32_t b = (uint32_t)(z.extra + 32);
+        if (z.has_extra && !(s_marks[b >> 5] >> (b & 31) & 1))
+            dz[z.skip + z.extra] = (T)(none ? 0.f : cq * __builtin_amdgcn_exp2f((z.extra_z - z_top) * k));
     }
 }
 
-template <typename T, int WHAT> static void launch_distill_as(const DistillArgs &a, hipStream_t stream) {
-    const uint32_t lds = WHAT & kDistillGradient ? (uint32_t)((a.vocab + 31) / 32) * 8 : 0;
-    hipLaunchKernelGGL((distill_kernel<T, WHAT>), dim3((uint32_t)a.rows), dim3(kDistillThreads), lds, stream, a);
+template <typename T, int WHAT, int THREADS, int HELD> static void launch_distill_as(const DistillArgs &a, hipStream_t stream) {
+    const int32_t part = WHAT == kDistillGradient ? a.part : a.vocab;
+    const uint32_t lds = WHAT & kDistillGradient ? (uint32_t)mark_words(part) * 8 : 0;
+    hipLaunchKernelGGL((distill_kernel<T, WHAT, THREADS, HELD>), dim3((uint32_t)a.rows, (uint32_t)((a.vocab + part - 1) / part)), dim3(THREADS), lds,
+                       stream, a);
+}
+
+template <typename T> static void launch_distill_loss(const DistillArgs &a, hipStream_t stream) {
+    if (a.rows >= 8 * kCus && a.vocab <= 4096) launch_distill_as<T, kDistillLoss, 64, 0>(a, stream);
+    else if (a.rows >= 8 * kCus) launch_distill_as<T, kDistillLoss, 256, 0>(a, stream);
+    else if (a.rows >= 4 * kCus) launch_distill_as<T, kDistillLoss, 512, 0>(a, stream);
+    else launch_distill_as<T, kDistillLoss, 1024, 0>(a, stream);
+}
+
+template <typename T> static void launch_distill_gradient(DistillArgs a, hipStream_t stream) {
+    a.part = 65536;
+    while (a.part / 2 >= a.vocab) a.part /= 2;
+    while (a.part > 4096 && (int64_t)a.rows * ((a.vocab + a.part - 1) / a.part) < 8 * kCus) a.part /= 2;
+    if (a.rows >= 8 * kCus && a.vocab <= 4096) launch_distill_as<T, kDistillGradient, 64, 0>(a, stream);
+    else launch_distill_as<T, kDistillGradient, 256, 0>(a, stream);
+}
+
+template <typename T> static void launch_distill_both(const DistillArgs &a, hipStream_t stream) {
+    constexpr int kBoth = kDistillLoss | kDistillGradient;
+    constexpr int64_t kPer = 16 / sizeof(T);
+    if (a.rows <= kCus) {  // a row per CU: as many threads as it takes
+        if (a.vocab <= 1024 * 4 * kPer) launch_distill_as<T, kBoth, 1024, 4>(a, stream);
+        else launch_distill_as<T, kBoth, 1024, 16>(a, stream);
+    } else if (a.vocab <= 64 * 4 * kPer) launch_distill_as<T, kBoth, 64, 4>(a, stream);
+    else if (a.vocab <= 256 * 4 * kPer) launch_distill_as<T, kBoth, 256, 4>(a, stream);
+    else if (a.vocab <= 256 * 16 * kPer) launch_distill_as<T, kBoth, 256, 16>(a, stream);
+    else if (a.vocab <= 512 * 16 * kPer) launch_distill_as<T, kBoth, 512, 16>(a, stream);
+    else launch_distill_as<T, kBoth, 512, 20>(a, stream);
 }
 
 scorch_status_t launch_distill(int what, int32_t rows, int32_t vocab, const void *Z, int32_t z_type, int64_t ldz, const int32_t *rowptr,
                                const int32_t *colidx, const float *vals, float x, const float *dloss, float *loss, float *stats,
                                void *dZ, int64_t lddz, hipStream_t stream) {
-    const DistillArgs a{Z, dZ, rowptr, colidx, vals, dloss, loss, stats, ldz, lddz, rows, vocab, x};
-    if (!grid_fits(rows, kDistillThreads)) {
+    const DistillArgs a{Z, dZ, rowptr, colidx, vals, dloss, loss, stats, ldz, lddz, rows, vocab, x, 0};
+    if (!grid_fits(rows, 1024)) {
         set_error("distillation: %d rows need a larger launch than HIP takes", rows);
         return SCORCH_ERR_UNSUPPORTED;
     }
     const bool ok = with_type(z_type, [&](auto tz) {
         typedef typename decltype(tz)::type T;
-        if (what == kDistillLoss) launch_distill_as<T, kDistillLoss>(a, stream);
-        else if (what == kDistillGradient) launch_distill_as<T, kDistillGradient>(a, stream);
-        else launch_distill_as<T, kDistillLoss | kDistillGradient>(a, stream);
+        if (what == kDistillLoss) launch_distill_loss<T>(a, stream);
+        else if (what == kDistillGradient) launch_distill_gradient<T>(a, stream);
+        else launch_distill_both<T>(a, stream);
     });
     if (!ok) {
         set_error("distillation: unknown type %d", z_type);

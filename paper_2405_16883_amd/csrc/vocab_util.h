@@ -2,6 +2,7 @@
 #pragma once
 
 #include <math.h>
+#include <type_traits>
 
 #include "spmm_internal.h"
 
@@ -27,6 +28,21 @@ template <typename T, int N> __device__ __forceinline__ void load_floats_part(co
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = i < n ? (float)p[i] : rest;
 }
+// 16 bytes as they are in memory, for values that stay in registers: a vector of 16-bit types is kept as a register per element by the compiler.
+typedef uint32_t raw16 __attribute__((ext_vector_type(4)));
+typedef uint32_t raw16_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t raw16_at2 __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T> __device__ __forceinline__ raw16 load_raw16(const T *p) {
+    return *reinterpret_cast<const std::conditional_t<sizeof(T) == 4, raw16_at4, raw16_at2> *>(p);
+}
+// Element i of them as a float.
+template <typename T> __device__ __forceinline__ float element(const raw16 &v, int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[i]);
+    const uint32_t pair = v[i / 2];
+    if constexpr (std::is_same_v<T, bf16>) return __uint_as_float(i % 2 ? pair & 0xffff0000u : pair << 16);
+    return (float)__builtin_bit_cast(f16, (uint16_t)(i % 2 ? pair >> 16 : pair));
+}
+
 // N floats, rounded to the nearest T (ties to even), the only rounding on the way to a 16-bit result.
 template <typename T, int N, bool NT = false> __device__ __forceinline__ void store_floats(T *p, const float (&x)[N]) {
     typename Pack<T, N>::type v;
