@@ -399,7 +399,7 @@ template <typename TE> __device__ __forceinline__ void fill_rows(const RunArgs &
 }
 
 // N consecutive elements, the first `left` of them if there are fewer.
-template <typename T, int N> __device__ __forceinline__ typename Pack<T, N>::type load_raw(const T *p, int left) {
+template <typename T, int N> __device__ __forceinline__ typename Pack<T, N>::type load_some(const T *p, int left) {
     typename Pack<T, N>::type v = {};
     if (left >= N) {
         v = *reinterpret_cast<const typename Pack<T, N>::type *>(p);
@@ -472,10 +472,10 @@ __global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
 #pragma unroll
             for (int u = 0; u < LOADS; ++u) {
                 const int e = std::min(e0 + u, n - 1);
-                x[u] = load_raw<TD, N>(src + __builtin_amdgcn_readlane(my_row, e) * a.lddo, left);
+                x[u] = load_some<TD, N>(src + __builtin_amdgcn_readlane(my_row, e) * a.lddo, left);
                 if constexpr (ADD) {
                     const int32_t key = __builtin_amdgcn_readlane(my_key, e);
-                    if (last >> e & 1 && key < a.vocab) old[u] = load_raw<TE, N>(dst + key * a.ldde, left);
+                    if (last >> e & 1 && key < a.vocab) old[u] = load_some<TE, N>(dst + key * a.ldde, left);
                 }
             }
 #pragma unroll
@@ -538,7 +538,7 @@ __global__ __launch_bounds__(kJoinThreads) void run_join_kernel(const RunArgs a)
     auto finish = [&](int32_t id, float (&acc)[N]) {
         if (left <= 0) return;
         typename Pack<TE, N>::type old = {};
-        if constexpr (ADD) old = load_raw<TE, N>(static_cast<const TE *>(a.dE) + id * a.ldde + c0, left);
+        if constexpr (ADD) old = load_some<TE, N>(static_cast<const TE *>(a.dE) + id * a.ldde + c0, left);
         store_row<TE, N, ADD>(a, id, c0, left, acc, old);
     };
     const int32_t n_runs = a.long_runs[0];

@@ -32,8 +32,19 @@ template <typename T, int N> __device__ __forceinline__ void load_floats_part(co
 typedef uint32_t raw16 __attribute__((ext_vector_type(4)));
 typedef uint32_t raw16_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t raw16_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t raw8_at4 __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t raw8_at2 __attribute__((ext_vector_type(2), aligned(2)));
 template <typename T> __device__ __forceinline__ raw16 load_raw16(const T *p) {
     return *reinterpret_cast<const std::conditional_t<sizeof(T) == 4, raw16_at4, raw16_at2> *>(p);
+}
+// The first BYTES, 8 or 16, of them.
+template <typename T, int BYTES> __device__ __forceinline__ raw16 load_raw(const T *p) {
+    if constexpr (BYTES == 16) return load_raw16(p);
+    else {
+        typedef std::conditional_t<sizeof(T) == 4, raw8_at4, raw8_at2> at_element;
+        const at_element v = *reinterpret_cast<const at_element *>(p);
+        return raw16{v[0], v[1], 0, 0};
+    }
 }
 // Element i of them as a float.
 template <typename T> __device__ __forceinline__ float element(const raw16 &v, int i) {
