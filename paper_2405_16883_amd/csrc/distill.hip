@@ -83,8 +83,9 @@ template <typename T, int THREADS, int HELD> struct LogitRow {
         skip = std::min(vocab, (int32_t)(-reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)));
         z = row + skip;
         whole = (vocab - skip) / N * N;
-        has_extra = whole + (int)threadIdx.x < vocab;
-        extra = (int)threadIdx.x < skip ? (int)threadIdx.x - skip : whole + (int)threadIdx.x - skip;
+        const int32_t t = (int32_t)threadIdx.x;
+        has_extra = t < vocab - whole;  // neither side passes 32 bits, whatever vocab is
+        extra = !has_extra ? 0 : t < skip ? t - skip : whole + (t - skip);
         extra_z = has_extra ? (float)z[extra] : -INFINITY;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) held[u] = holds(u) ? load_raw16(mine(z, u)) : nothing();
@@ -120,10 +121,10 @@ template <typename T, int THREADS, int HELD> struct LogitRow {
         constexpr int U = HELD > 0 ? 8 / N : 4;  // vectors in flight
         top = extra_z == extra_z ? extra_z : -INFINITY;
         sum = extra_z == extra_z ? (extra_z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((extra_z - extra_z) * k)) : NAN;
-        for (int32_t j0 = HELD * kStep + (int)threadIdx.x * N; j0 < whole; j0 += U * kStep) {
+        for (int64_t j0 = HELD * kStep + (int)threadIdx.x * N; j0 < whole; j0 += U * kStep) {
             raw16 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = j0 + (int64_t)u * kStep < whole ? load_raw16(z + j0 + u * kStep) : nothing();
+            for (int u = 0; u < U; ++u) v[u] = j0 + u * kStep < whole ? load_raw16(z + j0 + u * kStep) : nothing();
             float m = top;
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
     Row z(static_cast<const T *>(a.Z) + row * a.ldz + lo, cols);
     const int32_t p0 = a.rowptr[row], p1 = a.rowptr[row + 1];
     const float k = a.x * kLog2e;
-    const int words = mark_words(cols);
+    const int words = kGradient ? mark_words(cols) : 0;
     uint32_t *s_twice = s_marks + words;
     auto bit_of = [&](int32_t col) { return (uint32_t)(col - z.skip + 32); };  // a vector's bits are in one word
     // An entry that counts as stored; col < 0 or >= cols: a column of another part.
@@ -176,17 +177,16 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
         bool stored;
     };
     auto read = [&](int32_t p) {
-        Entry e{p, 0, 0.f, 0.f, p < p1};
-        if (!e.stored) return e;
-        e.col = a.colidx[p];
-        e.t = a.vals[p];
+        Entry e{p, a.colidx[p], a.vals[p], 0.f, false};
         e.stored = (uint32_t)e.col < (uint32_t)a.vocab && e.t != -INFINITY;
         e.col -= lo;
         if (e.stored && (kLoss || (uint32_t)e.col < (uint32_t)cols)) e.z = (float)z.z[e.col - z.skip];
         return e;
     };
-    const Entry own = read(p0 + tid);  // most rows have no more than one per thread: read once
+    const bool any = tid < p1 - p0;
+    const Entry own = any ? read(p0 + tid) : Entry{};  // most rows have no more than one per thread: read once
     auto entries = [&](auto f) {
+        if (!any) return;
         if (own.stored) f(own);
         for (int32_t p = p0 + tid; p1 - p > THREADS;) {
             p += THREADS;
@@ -294,9 +294,9 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
 }
 
 template <typename T, int WHAT, int THREADS, int HELD> static void launch_distill_as(const DistillArgs &a, hipStream_t stream) {
-    const int32_t part = WHAT == kDistillGradient ? a.part : a.vocab;
+    const int32_t part = WHAT == kDistillGradient ? a.part : std::max(a.vocab, 1);
     const uint32_t lds = WHAT & kDistillGradient ? (uint32_t)mark_words(part) * 8 : 0;
-    hipLaunchKernelGGL((distill_kernel<T, WHAT, THREADS, HELD>), dim3((uint32_t)a.rows, (uint32_t)((a.vocab + part - 1) / part)), dim3(THREADS), lds,
+    hipLaunchKernelGGL((distill_kernel<T, WHAT, THREADS, HELD>), dim3((uint32_t)a.rows, WHAT == kDistillGradient ? (uint32_t)((a.vocab + part - 1) / part) : 1), dim3(THREADS), lds,
                        stream, a);
 }
 

@@ -148,12 +148,17 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs
 
 // The lanes of this wavefront that hold the same digit, of those that take part.
 __device__ __forceinline__ uint64_t same_digit(int digit, int bits, bool valid) {
-    uint64_t peers = __ballot(valid);
-    for (int b = 0; b < bits; ++b) {
-        const uint64_t set = __ballot(digit >> b & 1);
-        peers &= digit >> b & 1 ? set : ~set;
+    const uint64_t all = __ballot(valid);
+    uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+        if (b >= bits) break;
+        const uint32_t mine = (uint32_t)__builtin_amdgcn_sbfe(digit, b, 1);  // the bit, in all places
+        const uint64_t set = __ballot(mine != 0);
+        lo &= ~((uint32_t)set ^ mine);
+        hi &= ~((uint32_t)(set >> 32) ^ mine);
     }
-    return peers;
+    return (uint64_t)hi << 32 | lo;
 }
 
 // Exclusive sum over the threads of a workgroup of kSortThreads.
@@ -248,7 +253,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
 
 // For short lists: one launch, in which a workgroup has a range of ids and a part of the positions.  It reads the whole list, counts the ids of
 // its range and those below it, and so knows where its own go: no workgroup waits for another.
-constexpr int kRankBitsMax = 10;  // ids per range, in bits: 18 counters per id in LDS
+constexpr int kRankBitsMax = kDigitBits;  // ids per range, in bits: 18 counters per id in LDS
 constexpr int kRankRounds = 4;    // ids of its part that a thread holds, at most
 
 struct RankArgs {
@@ -683,6 +688,11 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
                                 int64_t lddo, float scale, int32_t accumulate, void *dE, int32_t de_type, int64_t ldde,
                                 char *workspace, hipStream_t stream) {
     const GradLayout l = layout_gradient(tokens, d);
+    const int64_t tiles = ((int64_t)d + kWave * 4 - 1) / (kWave * 4);  // of the wider type
+    if (!grid_fits(l.chunks * tiles / kWavesPerBlock + (int64_t)vocab / (4 * kWavesPerBlock) + 2, kBlock)) {
+        set_error("embedding gradient: %d tokens, %d ids and %d columns need a larger launch than HIP takes", tokens, vocab, d);
+        return SCORCH_ERR_UNSUPPORTED;
+    }
     const int32_t *keys = nullptr, *perm = nullptr;
     sort_by_id(tokens, vocab, ids, workspace, l, stream, keys, perm);
     RunArgs r{};
@@ -720,7 +730,7 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
                  auto launch = [&](auto add) {
                      constexpr bool ADD = decltype(add)::value;
                      if (sums.x > 0) hipLaunchKernelGGL((run_sum_kernel<TD, TE, N, ADD ? 4 : 8, ADD>), sums, dim3(kBlock), 0, stream, r);
-                     if (r.chunks > 2) hipLaunchKernelGGL((run_join_kernel<TE, ADD>), joins, dim3(kJoinThreads), 0, stream, r);
+                     if (r.chunks > 1) hipLaunchKernelGGL((run_join_kernel<TE, ADD>), joins, dim3(kJoinThreads), 0, stream, r);
                  };
                  if (accumulate) launch(std::true_type());
                  else launch(std::false_type());

@@ -243,8 +243,8 @@ scorch_status_t launch_logits(int32_t rows, int32_t vocab, const void *in, int32
                               void *out, int32_t out_type, int64_t ldo, hipStream_t stream) {
     LogitsArgs a{in, out, rules, ldi, ldo, rows, vocab, 0, 0, 0};
     a.tile = kLogitsThreads * kLogitsVectors * (type == SCORCH_TYPE_F32 || out_type == SCORCH_TYPE_F32 ? 4 : 8);  // kPer16 of the types
-    a.tiles = (vocab + a.tile - 1) / a.tile;
-    a.parts = std::min(a.tiles, (4 * kCus + rows - 1) / rows);  // twice what runs at once: two workgroups per CU
+    a.tiles = (int32_t)(((int64_t)vocab + a.tile - 1) / a.tile);
+    a.parts = std::min(a.tiles, std::max(1, 4 * kCus / rows));  // twice what runs at once: two workgroups per CU
     const int64_t grid = (int64_t)rows * a.parts;
     if (!grid_fits(grid, kLogitsThreads)) {
         set_error("logits: %d rows of %d columns need a larger launch than HIP takes", rows, vocab);

@@ -203,3 +203,37 @@ def test_replay_in_a_graph_on_another_stream():
         torch.cuda.synchronize()
         for x, y in zip((loss, stats, apart, both, dZ), want):
             assert torch.equal(x, y), f"replay {replay}"
+
+
+def test_a_row_as_long_as_an_index_goes():
+    vocab = 2 ** 31 - 1
+    Z = torch.zeros((1, vocab), dtype=torch.float16, device="cuda")
+    loss, stats = torch.empty(1, device="cuda"), torch.empty((1, 2), device="cuda")
+    rowptr = torch.tensor([0, 2], dtype=torch.int32, device="cuda")
+    cols = torch.tensor([vocab - 1, 5], dtype=torch.int32, device="cuda")
+    sp.scorch_distill_loss(Z, rowptr, cols, torch.tensor([1.0, 1.0], device="cuda"), 1.0, loss, stats)
+    # q = 1 / vocab, p = 1 / 2 twice; a thread adds 2^21 ones, exactly
+    assert abs(loss.item() - np.log(vocab / 2)) < 1e-5 and stats[0, 0] == 0 and abs(stats[0, 1].item() / vocab - 1) < 1e-6
+
+
+@pytest.mark.parametrize("vocab", [1, 5, 9, 100, 8191, 65536, 70001])
+def test_rows_at_every_alignment(vocab):
+    """Rows that begin at every element of a 16-byte vector, logits and gradient at different ones."""
+    Z, lists = problem(3, vocab, min(vocab, 20), vocab)
+    for kind in ("bf16", "f32"):
+        z = Z.to(TYPES[kind])
+        ref = run(z, lists, 1.0)[4]
+        rowptr, cols = csr([c for c, _ in lists])
+        _, vals = csr([t for _, t in lists])
+        cols, vals = torch.from_numpy(cols.astype(np.int32)).cuda(), torch.from_numpy(vals.astype(np.float32)).cuda()
+        for off in range(8):
+            a = torch.full((3 * (vocab + 8) + 8,), SENTINEL, dtype=z.dtype, device="cuda")
+            b = torch.full_like(a, SENTINEL)
+            src, dst = a[off:].as_strided((3, vocab), (vocab + off, 1)), b[7 - off:].as_strided((3, vocab), (vocab + 8 - off, 1))
+            src.copy_(z)
+            loss = torch.empty(3, device="cuda")
+            sp.scorch_distill_loss_gradient(src, rowptr, cols, vals, 1.0, None, loss, dst)
+            assert torch.allclose(dst.float(), ref.float(), rtol=1e-2 if kind == "bf16" else 1e-5, atol=1e-7)
+            written = torch.zeros_like(b, dtype=torch.bool)
+            written[7 - off:].as_strided((3, vocab), (vocab + 8 - off, 1)).fill_(True)
+            assert (b[~written] == SENTINEL).all()

@@ -164,3 +164,41 @@ def test_lookup_and_gradient_replay_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(dE, want_dE), f"replay {replay}"
+
+
+def test_gradient_of_two_chunks_and_a_run_over_both():
+    """Very wide rows: so many tiles of columns that 400 tokens are two chunks of 256 entries."""
+    tokens, d = 400, 1 << 22
+    dout = torch.randint(-2, 3, (tokens, d), device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    for ids in (torch.zeros(tokens), (torch.arange(tokens) >= 30).int(), (torch.arange(tokens) >= 250).int(), (torch.arange(tokens) >= 350).int()):
+        ids = ids.to(torch.int32).cuda()
+        dE = torch.full((2, d), float("nan"), device="cuda")
+        sp.scorch_embedding_gradient(ids, dout, dE)
+        for v in (0, 1):  # whole numbers: any order gives the same sums
+            want = torch.zeros(d, device="cuda")
+            for t in torch.nonzero(ids == v)[:, 0].tolist():
+                want += dout[t].float()
+            assert torch.equal(dE[v], want)
+
+
+@pytest.mark.parametrize("length", list(range(1, 40)) + [63, 64, 65, 127, 128, 129, 300, 511, 513, 1500])
+def test_gradient_of_runs_of_one_length(length):
+    """Runs end at every place of a chunk, and reach over one, two or many."""
+    tokens, d = 2048, 24
+    ids = (torch.arange(tokens) // length).to(torch.int32).cuda()
+    check_gradient(ids, int(ids[-1]) + 2, d, "bf16", "f32", False, scale=1.0, integers=True)
+    check_gradient(ids.flip(0).contiguous(), int(ids[0]) + 2, d, "f32", "f32", True, scale=1.0, integers=True)
+
+
+@pytest.mark.parametrize("length", [5, 31, 32, 33, 40, 64, 66, 96, 250, 3000])
+def test_gradient_of_runs_of_one_length_in_long_chunks(length):
+    """Enough tokens and columns that a chunk has 32 entries and more, and that runs may end a part of one behind it."""
+    tokens, d = 40000, 2049
+    ids = (torch.arange(tokens) // length).to(torch.int32).cuda()
+    ids = ids[torch.randperm(tokens, generator=torch.Generator().manual_seed(1)).cuda()].contiguous()
+    vocab = tokens // length + 3
+    dout = torch.randint(-4, 5, (tokens, d), device="cuda").to(torch.bfloat16)
+    want = torch.zeros((vocab, d), device="cuda", dtype=torch.float64).index_add_(0, ids.long(), dout.double())
+    dE = torch.full((vocab, d), float("nan"), device="cuda")
+    sp.scorch_embedding_gradient(ids, dout, dE)
+    assert torch.equal(dE.double(), want)

@@ -157,3 +157,30 @@ def test_replay_in_a_graph_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want), f"replay {replay}"
+
+
+def test_a_row_as_long_as_an_index_goes():
+    vocab = 2 ** 31 - 1
+    x = torch.zeros((1, vocab), dtype=torch.float16, device="cuda")
+    history = torch.tensor([vocab - 1, 7, vocab - 1], dtype=torch.int32, device="cuda")
+    rowptr = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    one = torch.ones(1, device="cuda")
+    sp.scorch_logits_process(x, x, rowptr, history, frequency=one, bias_rowptr=rowptr, bias_tokens=history, bias_vals=torch.tensor([5.0, 3.0, 0.5], device="cuda"))
+    assert x[0, vocab - 1] == 3.5 and x[0, 7] == 2 and x.count_nonzero() == 2
+
+
+@pytest.mark.parametrize("rows", [1, 2, 5, 33, 130, 520, 1100])
+def test_all_numbers_of_tiles_per_workgroup(rows):
+    """More rows, fewer workgroups per row: each works on up to all tiles of it."""
+    vocab = 50021
+    rng = np.random.default_rng(rows)
+    c = case(min(rows, 6), vocab, 300, 60, rows)
+    c = {k: (v[np.arange(rows) % len(v)] if isinstance(v, np.ndarray) else [v[i % len(v)] for i in range(rows)]) for k, v in c.items()}
+    x = torch.randn((min(rows, 6), vocab), device="cuda").repeat(-(-rows // 6), 1)[:rows].contiguous()
+    out = torch.empty_like(x)
+    sp.scorch_logits_process(x, out, **arguments(c, rows))
+    few = {k: v[:6] for k, v in c.items()}
+    ref, tol = logits_ref(x[:6], **few)
+    assert_within(out[:6], ref, tol + U * np.abs(np.where(np.isfinite(ref), ref, 0)) + 1e-30)
+    for i in range(6, rows):
+        assert torch.equal(out[i], out[i % 6])
