@@ -284,7 +284,9 @@ scorch_status_t scorch_dcsr_to_csr_rowptr(int32_t m, int32_t n_stored_rows, cons
  * Dense operands are row-major with a row stride (ld...) in elements, of one of the types below; their base needs the alignment of an
  * element, no more.  Row strides are 64-bit, every offset is computed in 64 bits.  Sums and softmax statistics are held in 32 bits,
  * results of 16 bits are rounded once, to nearest.  Ids and columns outside [0, vocab) are legal and stand for nothing (padding).  The
- * order of every sum is fixed, so repeated calls give the same bits.  None of these calls waits or allocates.
+ * order of every sum is fixed, so repeated calls give the same bits.  None of these calls waits or allocates.  Sizes that need a larger
+ * launch than HIP takes (2^32 threads: some four million rows of logits) are SCORCH_ERR_UNSUPPORTED, and so are tables of more than
+ * 4 194 304 columns.
  */
 enum { SCORCH_TYPE_F32 = 0, SCORCH_TYPE_BF16 = 1, SCORCH_TYPE_F16 = 2 };
 

@@ -189,6 +189,18 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int bins = 1 << a.bits;
     int32_t *count = s_move + wv * bins;
+    const int64_t begin = blockIdx.x * a.part_len;
+    const int64_t end = std::min<int64_t>(begin + a.part_len, a.tokens);
+    int32_t key[ROUNDS], pos[ROUNDS], place[ROUNDS];
+    auto request = [&](int64_t step) {
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int64_t i = step + (int64_t)wv * kWave * ROUNDS + r * kWave + lane;  // a wavefront has consecutive positions
+            key[r] = i < end ? sort_key(a, i) : 0;
+            pos[r] = i < end && a.perm_in ? a.perm_in[i] : (int32_t)i;
+        }
+    };
+    request(begin);  // under way while the places are worked out
     {
         // where this part's ids go: behind all of lower digits, and those of the same digit in earlier parts
         s_base[tid] = 0;
@@ -208,13 +220,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
         const int32_t lower = sort_scan(tid < bins ? s_total[tid] : 0, s_wave);
         if (tid < bins) s_base[tid] += lower;
     }
-    const int64_t begin = blockIdx.x * a.part_len;
-    const int64_t end = std::min<int64_t>(begin + a.part_len, a.tokens);
     for (int64_t step = begin; step < end; step += kSortThreads * ROUNDS) {
-        int32_t key[ROUNDS], place[ROUNDS];
-        const int64_t mine = step + (int64_t)wv * kWave * ROUNDS + lane;  // a wavefront has consecutive positions
-#pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) key[r] = mine + r * kWave < end ? sort_key(a, mine + r * kWave) : 0;
+        const int64_t mine = step + (int64_t)wv * kWave * ROUNDS + lane;
         for (int i = tid; i < kSortWaves * bins; i += kSortThreads) s_move[i] = 0;
         __syncthreads();
 #pragma unroll
@@ -244,9 +251,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
             if (i < end) {
                 const int32_t to = count[key[r] >> a.shift & (bins - 1)] + place[r];
                 a.keys_out[to] = key[r];
-                a.perm_out[to] = a.perm_in ? a.perm_in[i] : (int32_t)i;
+                a.perm_out[to] = pos[r];
             }
         }
+        if (end - step > kSortThreads * ROUNDS) request(step + kSortThreads * ROUNDS);
         __syncthreads();
     }
 }
@@ -509,42 +517,48 @@ __global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
     if (tail_here && unit % a.tiles == 0 && lane == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1)] = (int32_t)c;
 }
 
-// Adds up the runs that have partial rows, which are listed in any order.  A wavefront takes a run and 64 vectors of columns; if it has
-// more than a few partial rows, the wavefronts of the workgroup share it, in equal consecutive shares.
+// Adds up the runs that have partial rows, which are listed in any order.  A wavefront takes a run and 64 columns, 16 lanes a row, so that 32 rows are
+// in flight; if the run has more, the wavefronts of the workgroup share it, in equal consecutive shares.
 constexpr int kJoinThreads = 1024;
 constexpr int kJoinWaves = kJoinThreads / kWave;
-constexpr int kJoinLoads = 8;   // in flight
-constexpr int kJoinShort = 32;  // partial rows that are one wavefront's
+constexpr int kJoinLanes = 16;
+constexpr int kJoinColumns = 4 * kJoinLanes;
+constexpr int kJoinGroups = kWave / kJoinLanes;
+constexpr int kJoinLoads = 8;
+constexpr int kJoinShort = kJoinGroups * kJoinLoads;  // partial rows that are one wavefront's
 
 template <typename TE, bool ADD>
 __global__ __launch_bounds__(kJoinThreads) void run_join_kernel(const RunArgs a) {
     constexpr int N = 4;
-    __shared__ float s_acc[kJoinWaves][kWave][N];
+    __shared__ float s_acc[kJoinWaves][kJoinLanes][N];
     __shared__ int64_t s_rows[kJoinWaves];
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int c0 = ((int)blockIdx.y * kWave + lane) * N;
+    const int col = lane % kJoinLanes, group = lane / kJoinLanes;
+    const int c0 = (int)blockIdx.y * kJoinColumns + col * N;
     const int left = a.d - c0;
-    // partial rows k in [from, to) of the run that begins in chunk c: the end of c, then the beginnings of c + 1, ...
+    // partial rows k in [from, to) of the run that begins in chunk c: the end of c, then the beginnings of c + 1, ...; the sum in all groups
     auto add = [&](int64_t c, int64_t from, int64_t to, float (&acc)[N]) {
-        if (left <= 0) return;
-        for (int64_t k0 = from; k0 < to; k0 += kJoinLoads) {
-            float x[kJoinLoads][N];
+        if (left > 0)
+            for (int64_t k0 = from; k0 < to; k0 += kJoinShort) {
+                float x[kJoinLoads][N];
 #pragma unroll
-            for (int u = 0; u < kJoinLoads; ++u) {
-                const int64_t k = std::min(k0 + u, to - 1);
-                load_floats(a.partials + ((c + k) * 2 + (k == 0)) * a.stride + c0, x[u]);  // rows of partials are padded
+                for (int u = 0; u < kJoinLoads; ++u) {
+                    const int64_t k = std::min(k0 + u * kJoinGroups + group, to - 1);
+                    load_floats(a.partials + ((c + k) * 2 + (k == 0)) * a.stride + c0, x[u]);  // rows of partials are padded
+                }
+#pragma unroll
+                for (int u = 0; u < kJoinLoads; ++u)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] += k0 + u * kJoinGroups + group < to ? x[u][j] : 0.f;
             }
 #pragma unroll
-            for (int u = 0; u < kJoinLoads; ++u)
-#pragma unroll
-                for (int j = 0; j < N; ++j) acc[j] += k0 + u < to ? x[u][j] : 0.f;
+        for (int j = 0; j < N; ++j) {
+            acc[j] += lane_xor<16>(acc[j]);
+            acc[j] += lane_xor<32>(acc[j]);
         }
     };
-    auto finish = [&](int32_t id, float (&acc)[N]) {
-        if (left <= 0) return;
-        typename Pack<TE, N>::type old = {};
-        if constexpr (ADD) old = load_some<TE, N>(static_cast<const TE *>(a.dE) + id * a.ldde + c0, left);
-        store_row<TE, N, ADD>(a, id, c0, left, acc, old);
+    auto held = [&](int32_t id) {  // requested before the partial rows
+        return ADD ? load_some<TE, N>(static_cast<const TE *>(a.dE) + id * a.ldde + c0, left) : typename Pack<TE, N>::type{};
     };
     const int32_t n_runs = a.long_runs[0];
     // neighbours in the list, often long runs next to each other, go to different workgroups
@@ -565,8 +579,9 @@ __global__ __launch_bounds__(kJoinThreads) void run_join_kernel(const RunArgs a)
             }
             if (rows <= kJoinShort) {
                 float acc[N] = {};
+                const auto old = held(id);
                 add(c, 0, rows, acc);
-                finish(id, acc);
+                if (left > 0 && group == 0) store_row<TE, N, ADD>(a, id, c0, left, acc, old);
                 rows = 0;
             }
         }
@@ -576,16 +591,20 @@ __global__ __launch_bounds__(kJoinThreads) void run_join_kernel(const RunArgs a)
             const int64_t n = s_rows[w];
             if (n == 0) continue;
             const int64_t c = a.long_runs[1 + first + (int64_t)w * gridDim.x];
+            const int32_t id = a.keys[(c + 1) * a.chunk];
             float acc[N] = {};
+            typename Pack<TE, N>::type old = {};
+            if (wv == 0) old = held(id);
             add(c, n * wv / kJoinWaves, n * (wv + 1) / kJoinWaves, acc);
+            if (group == 0)
 #pragma unroll
-            for (int j = 0; j < N; ++j) s_acc[wv][lane][j] = acc[j];
+                for (int j = 0; j < N; ++j) s_acc[wv][col][j] = acc[j];
             __syncthreads();
             if (wv == 0) {
                 for (int o = 1; o < kJoinWaves; ++o)
 #pragma unroll
-                    for (int j = 0; j < N; ++j) acc[j] += s_acc[o][lane][j];
-                finish(a.keys[(c + 1) * a.chunk], acc);
+                    for (int j = 0; j < N; ++j) acc[j] += s_acc[o][col][j];
+                if (left > 0 && group == 0) store_row<TE, N, ADD>(a, id, c0, left, acc, old);
             }
             __syncthreads();
         }
@@ -726,7 +745,8 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
                      while (r.fill_rows < kFillRowsMax && vocab / r.fill_rows > 8192) r.fill_rows *= 2;
                      fill = ((int64_t)vocab + r.fill_rows * kWavesPerBlock - 1) / (r.fill_rows * kWavesPerBlock);
                  }
-                 const dim3 sums((uint32_t)(r.reduce_blocks + fill)), joins((uint32_t)std::max(1, std::min((r.chunks + kJoinWaves - 1) / kJoinWaves, 2 * kCus / ((d + 255) / 256))), (uint32_t)((d + 255) / 256));
+                 const int32_t column_tiles = (d + kJoinColumns - 1) / kJoinColumns;
+                 const dim3 sums((uint32_t)(r.reduce_blocks + fill)), joins((uint32_t)std::max(1, std::min((r.chunks + kJoinWaves - 1) / kJoinWaves, 2 * kCus / column_tiles)), (uint32_t)column_tiles);
                  auto launch = [&](auto add) {
                      constexpr bool ADD = decltype(add)::value;
                      if (sums.x > 0) hipLaunchKernelGGL((run_sum_kernel<TD, TE, N, ADD ? 4 : 8, ADD>), sums, dim3(kBlock), 0, stream, r);

@@ -20,7 +20,7 @@ scorch_status_t launch_distill(int what, int32_t rows, int32_t vocab, const void
 scorch_status_t launch_logits(int32_t rows, int32_t vocab, const void *in, int32_t type, int64_t ldi, const scorch_logits_rules_t &rules,
                               void *out, int32_t out_type, int64_t ldo, hipStream_t stream);
 
-constexpr int32_t kEmbeddingColumnsMax = 1 << 23;  // tiles of columns are the slow dimension of a launch
+constexpr int32_t kEmbeddingColumnsMax = 1 << 22;  // tiles of columns are the slow dimension of a launch
 
 static int type_bytes(int32_t type) { return type == SCORCH_TYPE_F32 ? 4 : type == SCORCH_TYPE_BF16 || type == SCORCH_TYPE_F16 ? 2 : 0; }
 
