@@ -5,6 +5,7 @@
 // through ctypes.  binding.py keeps the signatures, the error type and everything that is not on the hot path.
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -305,8 +306,18 @@ PyObject *embedding_gradient(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
     const float scale = a.number(3);
     const int32_t accumulate = a.i32(4);
     int64_t bytes = -1;
-    void *ws = a.list(5, at::kByte, "workspace", bytes);
+    void *ws = a.list(5, at::kByte, "workspace", bytes, true);
     void *s = a.stream(6);
+    at::Tensor own;  // in the order of the current stream, as what is allocated after it
+    if (a.ok && v[5] == Py_None) {
+        size_t need = 0;
+        if (v[6] != Py_None) a.fail(PyExc_TypeError, "a call on another stream needs its workspace");
+        else if (scorch_embedding_gradient_workspace_bytes(dout.rows, dE.rows, dE.cols, &need) == SCORCH_OK) {
+            own = at::empty({(int64_t)need}, THPVariable_Unpack(v[2]).options().dtype(at::kByte));
+            ws = own.data_ptr();
+            bytes = (int64_t)need;
+        }  // otherwise the call below says what is wrong
+    }
     if (a.ok && dout.cols != dE.cols) a.fail(PyExc_ValueError, "dout and dE have different numbers of columns");
     return status_of(a, [&] {
         return scorch_embedding_gradient(dout.rows, dE.rows, dE.cols, ids, dout.p, dout.type, dout.ld, scale, accumulate, dE.p, dE.type, dE.ld, ws,

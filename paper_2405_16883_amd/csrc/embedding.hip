@@ -347,7 +347,10 @@ __global__ __launch_bounds__(kSortThreads) void rank_sort_kernel(const RankArgs 
 // ------------------------------------------------------------------------------------------
 // gradient: sums of runs
 // ------------------------------------------------------------------------------------------
+constexpr int kFewTokens = 128;
+
 struct RunArgs {
+    const int32_t *ids;          // as they are; used instead of the sorted list of up to kFewTokens
     const int32_t *keys, *perm;  // sorted by id
     const void *dout;
     void *dE;
@@ -392,13 +395,13 @@ __device__ __forceinline__ int32_t first_of(const int32_t *keys, int32_t n, int3
 }
 
 // Rows without a token become zeros: a lane looks one id up, then the wavefront stores row by row.
-template <typename TE> __device__ __forceinline__ void fill_rows(const RunArgs &a, int64_t wave) {
+template <typename TE> __device__ __forceinline__ void fill_rows(const RunArgs &a, const int32_t *keys, int64_t wave) {
     const int lane = threadIdx.x & 63;
     const int64_t v0 = wave * a.fill_rows, v = v0 + lane;
     bool empty = false;
     if (lane < a.fill_rows && v < a.vocab) {
-        const int32_t p = first_of(a.keys, a.tokens, (int32_t)v);
-        empty = p == a.tokens || a.keys[p] != (int32_t)v;
+        const int32_t p = first_of(keys, a.tokens, (int32_t)v);
+        empty = p == a.tokens || keys[p] != (int32_t)v;
     }
     constexpr int M = 16 / sizeof(TE);
     const float zero[M] = {};
@@ -425,12 +428,32 @@ template <typename T, int N> __device__ __forceinline__ typename Pack<T, N>::typ
 }
 
 // N: columns per lane.  LOADS: rows of dout in flight per wavefront.  ADD: dE holds something already; the row a run ends in is requested with
-// the run's last row of dout, so that no sum waits for it.
-template <typename TD, typename TE, int N, int LOADS, bool ADD>
+// the run's last row of dout, so that no sum waits for it.  FEW: every workgroup sorts the ids itself, which saves a launch, and every run is
+// the wavefront's that it begins with, which saves another.
+template <typename TD, typename TE, int N, int LOADS, bool ADD, bool FEW>
 __global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
+    __shared__ int32_t s_keys[FEW ? kFewTokens : 1], s_perm[FEW ? kFewTokens : 1], s_ids[FEW ? kFewTokens : 1];
     const int lane = threadIdx.x & 63;
+    if constexpr (FEW) {
+        const int tid = threadIdx.x;
+        int32_t key = 0;
+        if (tid < a.tokens) {
+            key = a.ids[tid];
+            if ((uint32_t)key >= (uint32_t)a.vocab) key = a.vocab;
+            s_ids[tid] = key;
+        }
+        __syncthreads();
+        if (tid < a.tokens) {
+            int place = 0;
+            for (int j = 0; j < a.tokens; ++j) place += (s_ids[j] < key) | ((s_ids[j] == key) & (j < tid));
+            s_keys[place] = key;
+            s_perm[place] = tid;
+        }
+        __syncthreads();
+    }
+    const int32_t *keys = FEW ? s_keys : a.keys, *perm = FEW ? s_perm : a.perm;
     if ((int64_t)blockIdx.x >= a.reduce_blocks) {
-        fill_rows<TE>(a, ((int64_t)blockIdx.x - a.reduce_blocks) * kWavesPerBlock + (threadIdx.x >> 6));
+        fill_rows<TE>(a, keys, ((int64_t)blockIdx.x - a.reduce_blocks) * kWavesPerBlock + (threadIdx.x >> 6));
         return;
     }
     const int64_t unit = (int64_t)blockIdx.x * kWavesPerBlock + (threadIdx.x >> 6);
@@ -440,18 +463,18 @@ __global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
     const int left = a.d - c0;  // none if it is not positive
     const int64_t begin = c * a.chunk;
     const int64_t end = std::min<int64_t>(begin + a.chunk, a.tokens), ahead = std::min<int64_t>(end + a.ahead, a.tokens);
-    auto key_at = [&](int64_t i) { return i >= 0 && i < a.tokens ? a.keys[i] : -1; };
-    const int32_t head = a.keys[begin], tail = a.keys[end - 1];
+    auto key_at = [&](int64_t i) { return i >= 0 && i < a.tokens ? keys[i] : -1; };
+    const int32_t head = keys[begin], tail = keys[end - 1];
     if (head >= a.vocab) return;  // ids outside the table are the last of the list
     const bool head_earlier = key_at(begin - 1) == head;
     // A run belongs to the chunk that it begins in, if it does not reach far into the next one.
-    const bool head_taken = head_earlier && key_at(begin - a.chunk - 1) != head && key_at(begin + a.ahead) != head;
+    const bool head_taken = head_earlier && (FEW || (key_at(begin - a.chunk - 1) != head && key_at(begin + a.ahead) != head));
     const bool tail_here = tail < a.vocab && key_at(end) == tail && !(head_earlier && head == tail);  // begins here and goes on
-    const bool tail_whole = tail_here && key_at(ahead) != tail;
+    const bool tail_whole = tail_here && (FEW || key_at(ahead) != tail);
     int64_t stop = end;
     if (tail_whole)
         for (int64_t k = end + lane;; k += kWave) {
-            const uint64_t out = ~__ballot(k < ahead && a.keys[k] == tail);
+            const uint64_t out = ~__ballot(k < ahead && keys[k] == tail);
             stop += out ? __builtin_ctzll(out) : kWave;
             if (out) break;
         }
@@ -468,9 +491,9 @@ __global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
     bool began_here = !head_earlier;  // the current run
     for (int64_t base = begin; base < stop; base += kWave) {
         const int n = (int)std::min<int64_t>(kWave, stop - base);
-        const int32_t my_key = lane < n ? a.keys[base + lane] : a.vocab;
-        const int32_t my_next = lane < n && base + lane + 1 < a.tokens ? a.keys[base + lane + 1] : -1;
-        const int32_t my_row = lane < n ? a.perm[base + lane] : 0;
+        const int32_t my_key = lane < n ? keys[base + lane] : a.vocab;
+        const int32_t my_next = lane < n && base + lane + 1 < a.tokens ? keys[base + lane + 1] : -1;
+        const int32_t my_row = lane < n ? perm[base + lane] : 0;
         const uint64_t last = __ballot(my_key != my_next);  // of its run
         int e0 = 0;
         if (head_taken && !began_here) {
@@ -514,7 +537,7 @@ __global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
     // a run that goes on
     if (key_at(end) != tail || tail_whole || (head_taken && head == tail)) return;
     if (left > 0) part(tail_here ? partial + a.stride : partial);
-    if (tail_here && unit % a.tiles == 0 && lane == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1)] = (int32_t)c;
+    if (!FEW && tail_here && unit % a.tiles == 0 && lane == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1)] = (int32_t)c;
 }
 
 // Adds up the runs that have partial rows, which are listed in any order.  A wavefront takes a run and 64 columns, 16 lanes a row, so that 32 rows are
@@ -712,8 +735,9 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
         set_error("embedding gradient: %d tokens, %d ids and %d columns need a larger launch than HIP takes", tokens, vocab, d);
         return SCORCH_ERR_UNSUPPORTED;
     }
+    const bool few = tokens <= kFewTokens;
     const int32_t *keys = nullptr, *perm = nullptr;
-    sort_by_id(tokens, vocab, ids, workspace, l, stream, keys, perm);
+    if (!few) sort_by_id(tokens, vocab, ids, workspace, l, stream, keys, perm);
     RunArgs r{};
     r.keys = keys;
     r.perm = perm;
@@ -728,7 +752,8 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
     r.d = d;
     r.chunk = l.chunk;
     r.chunks = l.chunks;
-    r.ahead = std::max(8, l.chunk / 4);
+    r.ahead = few ? tokens : std::max(8, l.chunk / 4);
+    r.ids = ids;
     r.stride = l.stride;
     r.scale = scale;
     bool ok = true;
@@ -749,8 +774,11 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
                  const dim3 sums((uint32_t)(r.reduce_blocks + fill)), joins((uint32_t)std::max(1, std::min((r.chunks + kJoinWaves - 1) / kJoinWaves, 2 * kCus / column_tiles)), (uint32_t)column_tiles);
                  auto launch = [&](auto add) {
                      constexpr bool ADD = decltype(add)::value;
-                     if (sums.x > 0) hipLaunchKernelGGL((run_sum_kernel<TD, TE, N, ADD ? 4 : 8, ADD>), sums, dim3(kBlock), 0, stream, r);
-                     if (r.chunks > 1) hipLaunchKernelGGL((run_join_kernel<TE, ADD>), joins, dim3(kJoinThreads), 0, stream, r);
+                     constexpr int LOADS = ADD ? 4 : 8;
+                     if (sums.x == 0) return;
+                     if (few) hipLaunchKernelGGL((run_sum_kernel<TD, TE, N, LOADS, ADD, true>), sums, dim3(kBlock), 0, stream, r);
+                     else hipLaunchKernelGGL((run_sum_kernel<TD, TE, N, LOADS, ADD, false>), sums, dim3(kBlock), 0, stream, r);
+                     if (!few && r.chunks > 1) hipLaunchKernelGGL((run_join_kernel<TE, ADD>), joins, dim3(kJoinThreads), 0, stream, r);
                  };
                  if (accumulate) launch(std::true_type());
                  else launch(std::false_type());

@@ -202,3 +202,33 @@ def test_gradient_of_runs_of_one_length_in_long_chunks(length):
     dE = torch.full((vocab, d), float("nan"), device="cuda")
     sp.scorch_embedding_gradient(ids, dout, dE)
     assert torch.equal(dE.double(), want)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 8, 9, 17, 64, 65, 127, 128, 129, 200])
+@pytest.mark.parametrize("which", ["zipf", "one id", "two ids", "padding last", "all different"])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_few_tokens(tokens, which, accumulate):
+    """Few enough that one launch does it all; the run lengths go over several chunks."""
+    rng = np.random.default_rng(tokens)
+    ids = {"zipf": lambda: zipf(tokens, 300, rng, 0.1), "one id": lambda: torch.full((tokens,), 299), "two ids": lambda: torch.arange(tokens) % 2 * 7,
+           "padding last": lambda: torch.where(torch.arange(tokens) < tokens // 2, torch.arange(tokens) // 3, -1),
+           "all different": lambda: torch.randperm(300)[:tokens]}[which]().to(torch.int32).cuda()
+    check_gradient(ids, 300, 1030, "bf16", "f32", accumulate, scale=1.0, integers=True)
+    check_gradient(ids, 300, 7, "f32", "bf16", accumulate, pad=2)
+
+
+def test_gradient_allocates_its_workspace_inside_a_capture():
+    ids = torch.randint(0, 50, (3000,), device="cuda", dtype=torch.int32)
+    dout = torch.randn((3000, 40), device="cuda")
+    want, got = torch.empty((50, 40), device="cuda"), torch.empty((50, 40), device="cuda")
+    sp.scorch_embedding_gradient(ids, dout, want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sp.scorch_embedding_gradient(ids, dout, got)
+    for _ in range(3):
+        got.fill_(-3.0)
+        other = torch.randn(1 << 20, device="cuda").mul_(2)  # eager work between the replays
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
