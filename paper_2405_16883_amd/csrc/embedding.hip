@@ -379,7 +379,7 @@ __device__ __forceinline__ void store_row(const RunArgs &a, int32_t id, int c0, 
     float y[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) y[j] = ADD ? (float)old[j] + acc[j] * a.scale : acc[j] * a.scale;
-    if (left >= N) store_floats(dst, y);
+    if (left >= N) store_floats(dst, y);  // streaming stores: 3 % less to 11 % more time
     else store_floats_part(dst, left, y);
 }
 
@@ -734,15 +734,21 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
                                 int64_t lddo, float scale, int32_t accumulate, void *dE, int32_t de_type, int64_t ldde,
                                 char *workspace, hipStream_t stream) {
     const GradLayout l = layout_gradient(tokens, d);
-    const int64_t tiles = ((int64_t)d + kWave * 4 - 1) / (kWave * 4);  // of the wider type
-    if (!grid_fits(l.chunks * tiles / kWavesPerBlock + (int64_t)vocab / (4 * kWavesPerBlock) + 2, kBlock)) {
+    RunArgs r{};
+    int64_t fill = 0;  // workgroups that store zeros: some 8192 wavefronts, more for the largest tables
+    if (!accumulate) {
+        r.fill_rows = 4;
+        while (r.fill_rows < kFillRowsMax && vocab / r.fill_rows > 8192) r.fill_rows *= 2;
+        fill = ((int64_t)vocab + r.fill_rows * kWavesPerBlock - 1) / (r.fill_rows * kWavesPerBlock);
+    }
+    const int64_t tiles = ((int64_t)d + kWave * 4 - 1) / (kWave * 4);  // of 32 bits, the more
+    if (!grid_fits(l.chunks * tiles / kWavesPerBlock + 1 + fill, kBlock)) {
         set_error("embedding gradient: %d tokens, %d ids and %d columns need a larger launch than HIP takes", tokens, vocab, d);
         return SCORCH_ERR_UNSUPPORTED;
     }
     const bool few = tokens <= kFewTokens;
     const int32_t *keys = nullptr, *perm = nullptr;
     if (!few) sort_by_id(tokens, vocab, ids, workspace, l, stream, keys, perm);
-    RunArgs r{};
     r.keys = keys;
     r.perm = perm;
     r.dout = dout;
@@ -768,12 +774,6 @@ scorch_status_t launch_gradient(int32_t tokens, int32_t vocab, int32_t d, const 
                  constexpr int N = 16 / sizeof(TD);
                  r.tiles = (d + kWave * N - 1) / (kWave * N);
                  r.reduce_blocks = ((int64_t)r.chunks * r.tiles + kWavesPerBlock - 1) / kWavesPerBlock;
-                 int64_t fill = 0;
-                 if (!accumulate) {  // some 8192 wavefronts
-                     r.fill_rows = 4;
-                     while (r.fill_rows < kFillRowsMax && vocab / r.fill_rows > 8192) r.fill_rows *= 2;
-                     fill = ((int64_t)vocab + r.fill_rows * kWavesPerBlock - 1) / (r.fill_rows * kWavesPerBlock);
-                 }
                  const int32_t column_tiles = (d + kJoinColumns - 1) / kJoinColumns;
                  const dim3 sums((uint32_t)(r.reduce_blocks + fill)), joins((uint32_t)std::max(1, std::min((r.chunks + kJoinWaves - 1) / kJoinWaves, 2 * kCus / column_tiles)), (uint32_t)column_tiles);
                  auto launch = [&](auto add) {
