@@ -1,4 +1,5 @@
-"""MI355X-native CSR SpMM (C = A.B, A sparse CSR, B and C dense fp32) behind a C ABI.
+"""MI355X-native CSR SpMM (C = A.B, A sparse CSR, B and C dense fp32) behind a C ABI, and the operators of a language model's vocabulary in
+which lists of token ids meet dense rows.
 
 The product is libscorch_spmm.so (hand-written HIP for gfx950, see csrc/ and include/scorch_spmm.h);
 this package is its binding.

@@ -79,6 +79,7 @@ struct Args {
         if (!ok) return nullptr;
         const at::Tensor &t = THPVariable_Unpack(v[i]);
         if (!t.is_contiguous()) fail(PyExc_ValueError, "%s must be contiguous", name);
+        else if (t.is_neg()) fail(PyExc_ValueError, "%s is a negated view", name);
         else if (t.numel() > INT32_MAX) fail(PyExc_ValueError, "%s has too many elements", name);
         else if (n >= 0 && t.numel() != n) PyErr_Format(PyExc_ValueError, "%s must have %lld elements, got %lld", name, (long long)n, (long long)t.numel()), ok = false;
         else if (t.get_device() != c10::hip::current_device()) fail(PyExc_ValueError, "%s must live on the current device", name);
@@ -113,6 +114,7 @@ struct Args {
         else fail(PyExc_ValueError, "%s must be float32, bfloat16 or float16", name);
         if (!ok) return m;
         if (t.dim() != 2 || (t.numel() > 0 && t.size(1) > 1 && t.stride(1) != 1)) fail(PyExc_ValueError, "%s must be 2-D with unit column stride", name);
+        else if (t.is_neg()) fail(PyExc_ValueError, "%s is a negated view", name);
         else if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX) fail(PyExc_ValueError, "%s has too many rows or columns", name);
         else if (t.get_device() != c10::hip::current_device()) fail(PyExc_ValueError, "%s must live on the current device", name);
         if (!ok) return m;
