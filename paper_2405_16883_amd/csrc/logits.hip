@@ -4,7 +4,7 @@
 // Bound by the bytes of the logits read and written.  A workgroup has some tiles of columns of one row.  For a tile it counts in LDS how often
 // each token occurs in the row's history and looks the biases up there, with the tile's logits already on their way to registers; then it passes
 // over the tile once.  Counts are whole numbers, so the order of the atomic additions changes nothing.  Where a column has several biases, they are
-// added up in the order of the list.  256 rows of 131 072, bf16 to f32, histories of 2048, 64 biases, mask: 45 us, 60 when nothing is in a cache (a
+// added up in the order of the list.  256 rows of 131 072, bf16 to f32, histories of 2048, 64 biases, mask: 43 us, 57 when nothing is in a cache (a
 // plain copy 29 and 43); without biases 35.  33 rows of 50 257 with histories of 32 768 and 300 biases: 22 us, of which 12 go into biases
 // that repeat a token and 4 into the history, both on the one CU that has the row's most frequent tokens.
 #include "device_util.h"
@@ -241,12 +241,30 @@ __global__ __launch_bounds__(kLogitsThreads, 8) void logits_kernel(const LogitsA
     }
 }
 
+// Workgroups per row: those that take the fewest rounds of 2 per CU times tiles, counting a tile for a workgroup's start.  256 rows of 16 tiles: 2 parts 57 us,
+// 4 60, 8 63, 16 68.
+static int32_t row_parts(int32_t rows, int32_t tiles) {
+    const int64_t slots = 2 * kCus;
+    const int32_t most = (int32_t)std::min<int64_t>(tiles, std::max<int64_t>(1, 2 * slots / rows));
+    if (most > 64) return most;  // a few rows that are very long
+    int32_t best = 1;
+    int64_t least = INT64_MAX;
+    for (int32_t p = 1; p <= most; ++p) {
+        const int64_t cost = (rows * (int64_t)p + slots - 1) / slots * ((tiles + p - 1) / p + 1);
+        if (cost < least) {
+            least = cost;
+            best = p;
+        }
+    }
+    return best;
+}
+
 scorch_status_t launch_logits(int32_t rows, int32_t vocab, const void *in, int32_t type, int64_t ldi, const scorch_logits_rules_t &rules,
                               void *out, int32_t out_type, int64_t ldo, hipStream_t stream) {
     LogitsArgs a{in, out, rules, ldi, ldo, rows, vocab, 0, 0, 0};
     a.tile = kLogitsThreads * kLogitsVectors * (type == SCORCH_TYPE_F32 || out_type == SCORCH_TYPE_F32 ? 4 : 8);  // kPer16 of the types
     a.tiles = (int32_t)(((int64_t)vocab + a.tile - 1) / a.tile);
-    a.parts = std::min(a.tiles, std::max(1, 4 * kCus / rows));  // twice what runs at once, two per CU; one tile each: 53 us for 45
+    a.parts = row_parts(rows, a.tiles);
     const int64_t grid = (int64_t)rows * a.parts;
     if (!grid_fits(grid, kLogitsThreads)) {
         set_error("logits: %d rows of %d columns need a larger launch than HIP takes", rows, vocab);
