@@ -268,12 +268,17 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
             if ((uint32_t)e.col >= (uint32_t)cols) return;
             float prob = __builtin_amdgcn_exp2f((e.t - t_top) * k) * t_scale;
             if (s_twice[bit_of(e.col) >> 5] >> (bit_of(e.col) & 31) & 1) {
-                // the column's first entry adds the others up and is the only one to write there
+                // the column's first entry adds them all up, in their order, and is the only one to write there; the list is the same for all lanes
                 bool first = true;
-                for (int32_t o = p0; o < e.p && first; ++o) first = !(a.colidx[o] - lo == e.col && a.vals[o] != -INFINITY);
+                prob = 0.f;
+#pragma unroll 4
+                for (int32_t o = p0; o < p1; ++o) {
+                    const float t = a.vals[o];
+                    const bool same = (a.colidx[o] - lo == e.col) & (t != -INFINITY);
+                    first &= !same | (o >= e.p);
+                    prob += same ? __builtin_amdgcn_exp2f((t - t_top) * k) * t_scale : 0.f;
+                }
                 if (!first) return;
-                for (int32_t o = e.p + 1; o < p1; ++o)
-                    if (a.colidx[o] - lo == e.col && a.vals[o] != -INFINITY) prob += __builtin_amdgcn_exp2f((a.vals[o] - t_top) * k) * t_scale;
             }
             dz[e.col] = (T)(c * (__builtin_amdgcn_exp2f((e.z - z_top) * k) * q_scale - prob));
         });
