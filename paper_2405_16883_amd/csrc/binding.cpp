@@ -54,7 +54,7 @@ struct Args {
     float *floats(int i, const char *name) { return static_cast<float *>(ptr(i, at::kFloat, name)); }
 
     // Row stride of a matrix whose rows are contiguous.
-    int32_t ld(int i, const char *name) {
+    int64_t wide_ld(int i, const char *name) {
         if (!ok) return 0;
         if (!THPVariable_Check(v[i])) {
             PyErr_Format(PyExc_TypeError, "%s must be a tensor", name);
@@ -67,8 +67,9 @@ struct Args {
             ok = false;
             return 0;
         }
-        return (int32_t)(t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1)));
+        return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
     }
+    int32_t ld(int i, const char *name) { return (int32_t)wide_ld(i, name); }
 
     // A list of n int32 (or float) without gaps on the current device; n < 0: of any length, which is put there.  None: nullptr if that is
     // allowed.
@@ -409,7 +410,7 @@ PyObject *logits_process(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
     r.bias_vals = a.float_list(10, "bias_vals", entries, true);
     if (a.ok && v[11] != Py_None) {
         r.mask = reinterpret_cast<const uint32_t *>(a.ints(11, "mask"));
-        const int64_t ld = a.ld(11, "mask");
+        const int64_t ld = a.wide_ld(11, "mask");
         if (a.ok) {
             const at::Tensor &m = THPVariable_Unpack(v[11]);
             if (m.size(0) != x.rows || m.size(1) < ((int64_t)x.cols + 31) / 32) a.fail(PyExc_ValueError, "mask must have a row per row of logits and a bit per column");
