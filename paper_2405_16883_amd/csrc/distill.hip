@@ -4,7 +4,7 @@
 //     log sum_j exp(x z_j) = x M + log S,    M = max z_j,  S = sum_j exp(x (z_j - M)),    q_j = exp(x (z_j - M)) / S
 //
 // Bound by the bytes of the logits: the loss reads them once, the gradient reads and writes them.  A workgroup has a row.  Differences
-// from the largest logit are formed before they are scaled, so that nothing overflows where the result is a number.  Loss and gradient at once keep
+// from the largest logit are formed before they are scaled: nothing overflows where the result is a number.  Loss and gradient at once keep
 // the row in registers between the passes (maximum, sum, gradient), 16 or 20 vectors a thread with 16 wavefronts per CU: 81 920 16-bit columns, of
 // longer rows the rest is read again, mostly from the memory-side cache.  4096 rows of 131 072 bf16: 460 us, a copy of the same bytes 416; read
 // again throughout 543; fewer vectors and 32 wavefronts 568; a row per CU, held whole by 1024 threads, 505.  8192 rows of 32 000: 205 us, the copy 201.
@@ -34,6 +34,18 @@ struct DistillArgs {
     int32_t rows, vocab;
     float x;       // 1 / temperature
     int32_t part;  // the gradient alone: columns per workgroup, a power of two
+};
+
+// exp(x (v - top)) for v <= top.  v - top may pass the largest number, 3.4e38, where x times it does not; it then stands for a share of 0, which is right
+// while x times 3.4e38 is more than 102, as e^-102 is less than any number of 32 bits.  HALVES, for smaller x: differences of half the logits, which are
+// the same otherwise.  Not for all x, because it costs the fused call of 4096 rows of 131 072 1.5 %.
+constexpr float kHalvesBelow = 3e-37f;
+template <bool HALVES> struct Share {
+    float k;
+    __device__ __forceinline__ explicit Share(float x) : k(HALVES ? 2.f * (x * kLog2e) : x * kLog2e) {}
+    __device__ __forceinline__ float operator()(float v, float top) const {
+        return __builtin_amdgcn_exp2f((HALVES ? fmaf(v, 0.5f, -0.5f * top) : v - top) * k);
+    }
 };
 
 struct Max {
@@ -119,12 +131,12 @@ template <typename T, int THREADS, int HELD> struct LogitRow {
         }
         for (int32_t j = HELD * kStep + j0; j < whole; j += kStep) f(j, to + j, load_raw16(z + j));
     }
-    // The largest logit of this thread among those that are not held, and the sum of exp2((z - largest) k) over them; not a number if there is
+    // The largest logit of this thread among those that are not held, and the sum of the shares relative to it over them; not a number if there is
     // one that is not.
-    __device__ __forceinline__ void sum_with_max(float k, float &top, float &sum) const {
+    template <typename SHARE> __device__ __forceinline__ void sum_with_max(SHARE share, float &top, float &sum) const {
         constexpr int U = HELD > 0 ? 8 / N : 4;  // vectors in flight
         top = extra_z == extra_z ? extra_z : -INFINITY;
-        sum = extra_z == extra_z ? (extra_z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((extra_z - extra_z) * k)) : NAN;
+        sum = extra_z == extra_z ? (extra_z == -INFINITY ? 0.f : share(extra_z, extra_z)) : NAN;
         for (int64_t j0 = HELD * kStep + (int)threadIdx.x * N; j0 < whole; j0 += U * kStep) {
             raw16 v[U];
 #pragma unroll
@@ -142,12 +154,12 @@ template <typename T, int THREADS, int HELD> struct LogitRow {
                         if (element<T>(v[u], i) != element<T>(v[u], i)) sum = NAN;
                 continue;
             }
-            sum *= __builtin_amdgcn_exp2f((top - m) * k);
+            sum *= share(top, m);
             top = m;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum += __builtin_amdgcn_exp2f((element<T>(v[u], i) - m) * k);
+                for (int i = 0; i < N; ++i) sum += share(element<T>(v[u], i), m);
         }
     }
 };
@@ -156,7 +168,7 @@ template <typename T, int THREADS, int HELD> struct LogitRow {
 __host__ __device__ constexpr int mark_words(int32_t cols) { return (cols + 31) / 32 + 1; }
 
 // A workgroup has a row (the gradient alone: `part` columns of one, blockIdx.y-th).
-template <typename T, int WHAT, int THREADS, int HELD>
+template <typename T, int WHAT, int THREADS, int HELD, bool HALVES>
 __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(const DistillArgs a) {
     typedef LogitRow<T, THREADS, HELD> Row;
     constexpr int N = Row::N;
@@ -170,7 +182,7 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
     const int32_t cols = kLoss ? a.vocab : std::min(a.part, a.vocab - lo);
     Row z(static_cast<const T *>(a.Z) + row * a.ldz + lo, cols);
     const int32_t p0 = a.rowptr[row], p1 = a.rowptr[row + 1];
-    const float k = a.x * kLog2e;
+    const Share<HALVES> share(a.x);
     const int words = kGradient ? mark_words(cols) : 0;
     uint32_t *s_twice = s_marks + words;
     auto bit_of = [&](int32_t col) { return (uint32_t)(col - z.skip + 32); };  // a vector's bits are in one word
@@ -214,7 +226,7 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
     // largest logits, of the student's row and of the stored entries, then the sums
     float top = -INFINITY, sum = 0.f, z_top = 0.f;
     if constexpr (kLoss) {
-        z.sum_with_max(k, top, sum);
+        z.sum_with_max(share, top, sum);
         z_top = top;
 #pragma unroll
         for (int u = 0; u < HELD; ++u)
@@ -225,18 +237,18 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
     z.forget_floats();
     block_all(z_top, t_top, Max(), s_red[0]);
     if constexpr (kLoss) {
-        sum = top == -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((top - z_top) * k);
+        sum = top == -INFINITY ? sum : sum * share(top, z_top);
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             if (z.holds(u))
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum += __builtin_amdgcn_exp2f((element<T>(z.held[u], i) - z_top) * k);
+                for (int i = 0; i < N; ++i) sum += share(element<T>(z.held[u], i), z_top);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
     z.forget_floats();
     float t_sum = 0.f;
-    entries([&](const Entry &e) { t_sum += __builtin_amdgcn_exp2f((e.t - t_top) * k); });
+    entries([&](const Entry &e) { t_sum += share(e.t, t_top); });
     block_all(sum, t_sum, Sum(), s_red[1]);
     const bool none = t_sum == 0.f;  // otherwise the largest entry's share is 1, or something is not a number
     if constexpr (!kLoss) {
@@ -248,8 +260,10 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
         const float log_sums = logf(t_sum) - logf(sum);
         float divergence = 0.f, unused = 0.f;
         entries([&](const Entry &e) {
-            const float prob = __builtin_amdgcn_exp2f((e.t - t_top) * k) * t_scale;
-            if (prob != 0.f) divergence += prob * (a.x * (e.t - t_top) - a.x * (e.z - z_top) - log_sums);
+            const float prob = share(e.t, t_top) * t_scale;
+            // prob x ((t - t_top) - (z - z_top)) - prob log_sums, in an order in which only the product itself can pass the largest number or vanish
+            const float apart = fmaf(e.t, 0.5f, -0.5f * t_top) - fmaf(e.z, 0.5f, -0.5f * z_top);
+            if (prob != 0.f) divergence += 2.f * (apart * fminf(a.x, 1.f) * (prob * fmaxf(a.x, 1.f))) - prob * log_sums;
         });
         block_all(divergence, unused, Sum(), s_red[2]);
         if (tid == 0) {
@@ -266,7 +280,7 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
         const float q_scale = 1.f / sum, cq = c * q_scale;
         entries([&](const Entry &e) {
             if ((uint32_t)e.col >= (uint32_t)cols) return;
-            float prob = __builtin_amdgcn_exp2f((e.t - t_top) * k) * t_scale;
+            float prob = share(e.t, t_top) * t_scale;
             if (s_twice[bit_of(e.col) >> 5] >> (bit_of(e.col) & 31) & 1) {
                 // the column's first entry adds them all up, in their order, and is the only one to write there; the list is the same for all lanes
                 bool first = true;
@@ -276,18 +290,18 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
                     const float t = a.vals[o];
                     const bool same = (a.colidx[o] - lo == e.col) & (t != -INFINITY);
                     first &= !same | (o >= e.p);
-                    prob += same ? __builtin_amdgcn_exp2f((t - t_top) * k) * t_scale : 0.f;
+                    prob += same ? share(t, t_top) * t_scale : 0.f;
                 }
                 if (!first) return;
             }
-            dz[e.col] = (T)(c * (__builtin_amdgcn_exp2f((e.z - z_top) * k) * q_scale - prob));
+            dz[e.col] = (T)(c * (share(e.z, z_top) * q_scale - prob));
         });
         // Streaming stores: written once, and the memory-side cache is left to the logits that are read again
         z.each(dz + z.skip, [&](int32_t j, T *to, const raw16 &v) {
             const uint32_t marks = s_marks[(j >> 5) + 1] >> (j & 31) & ((1u << N) - 1);
             float y[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = none ? 0.f : cq * __builtin_amdgcn_exp2f((element<T>(v, i) - z_top) * k);
+            for (int i = 0; i < N; ++i) y[i] = none ? 0.f : cq * share(element<T>(v, i), z_top);
             if (marks == 0) {
                 store_floats<T, N, true>(to, y);
             } else {
@@ -298,21 +312,22 @@ __global__ __launch_bounds__(THREADS, HELD > 4 ? 4 : 8) void distill_kernel(cons
         });
         const uint32_t b = (uint32_t)(z.extra + 32);
         if (z.has_extra && !(s_marks[b >> 5] >> (b & 31) & 1))
-            dz[z.skip + z.extra] = (T)(none ? 0.f : cq * __builtin_amdgcn_exp2f((z.extra_z - z_top) * k));
+            dz[z.skip + z.extra] = (T)(none ? 0.f : cq * share(z.extra_z, z_top));
     }
 }
 
-template <typename T, int WHAT, int THREADS, int HELD> static void launch_distill_as(const DistillArgs &a, hipStream_t stream) {
+template <typename T, int WHAT, int THREADS, int HELD, bool HALVES = false> static void launch_distill_as(const DistillArgs &a, hipStream_t stream) {
     const int32_t part = WHAT == kDistillGradient ? a.part : std::max(a.vocab, 1);
     const uint32_t lds = WHAT & kDistillGradient ? (uint32_t)mark_words(part) * 8 : 0;
-    hipLaunchKernelGGL((distill_kernel<T, WHAT, THREADS, HELD>), dim3((uint32_t)a.rows, WHAT == kDistillGradient ? (uint32_t)((a.vocab + part - 1) / part) : 1), dim3(THREADS), lds,
+    hipLaunchKernelGGL((distill_kernel<T, WHAT, THREADS, HELD, HALVES>), dim3((uint32_t)a.rows, WHAT == kDistillGradient ? (uint32_t)((a.vocab + part - 1) / part) : 1), dim3(THREADS), lds,
                        stream, a);
 }
 
 // Threads per row: as many as fill the chip.  1 row of 131 072: 1024 threads 10 us, 256 threads 15; 2048 rows of 32 000: 256 threads 24 us.  Short rows of
 // many: a wavefront each (8192 rows of 1000: 7 us, 256 threads 17).
 template <typename T> static void launch_distill_loss(const DistillArgs &a, hipStream_t stream) {
-    if (a.rows >= 8 * kCus && a.vocab <= 4096) launch_distill_as<T, kDistillLoss, 64, 0>(a, stream);
+    if (a.x < kHalvesBelow) launch_distill_as<T, kDistillLoss, 1024, 0, true>(a, stream);
+    else if (a.rows >= 8 * kCus && a.vocab <= 4096) launch_distill_as<T, kDistillLoss, 64, 0>(a, stream);
     else if (a.rows >= 8 * kCus) launch_distill_as<T, kDistillLoss, 256, 0>(a, stream);
     else if (a.rows >= 4 * kCus) launch_distill_as<T, kDistillLoss, 512, 0>(a, stream);
     else launch_distill_as<T, kDistillLoss, 1024, 0>(a, stream);
@@ -324,7 +339,8 @@ template <typename T> static void launch_distill_gradient(DistillArgs a, hipStre
     a.part = 65536;
     while (a.part / 2 >= a.vocab) a.part /= 2;
     while (a.part > 4096 && (int64_t)a.rows * ((a.vocab + a.part - 1) / a.part) < 8 * kCus) a.part /= 2;
-    if (a.rows >= 8 * kCus && a.vocab <= 4096) launch_distill_as<T, kDistillGradient, 64, 0>(a, stream);
+    if (a.x < kHalvesBelow) launch_distill_as<T, kDistillGradient, 256, 0, true>(a, stream);
+    else if (a.rows >= 8 * kCus && a.vocab <= 4096) launch_distill_as<T, kDistillGradient, 64, 0>(a, stream);
     else launch_distill_as<T, kDistillGradient, 256, 0>(a, stream);
 }
 
@@ -333,7 +349,9 @@ template <typename T> static void launch_distill_gradient(DistillArgs a, hipStre
 template <typename T> static void launch_distill_both(const DistillArgs &a, hipStream_t stream) {
     constexpr int kBoth = kDistillLoss | kDistillGradient;
     constexpr int64_t kPer = 16 / sizeof(T);
-    if (a.rows <= kCus) {  // a row per CU: as many threads as it takes
+    if (a.x < kHalvesBelow) {
+        launch_distill_as<T, kBoth, 1024, 0, true>(a, stream);
+    } else if (a.rows <= kCus) {  // a row per CU: as many threads as it takes
         if (a.vocab <= 1024 * 4 * kPer) launch_distill_as<T, kBoth, 1024, 4>(a, stream);
         else launch_distill_as<T, kBoth, 1024, 16>(a, stream);
     } else if (a.vocab <= 64 * 4 * kPer) launch_distill_as<T, kBoth, 64, 4>(a, stream);
