@@ -322,7 +322,7 @@ scorch_status_t scorch_embedding_gradient_workspace_bytes(int32_t tokens, int32_
  * Z: rows x vocab.  Entries of a row may be in any order and may repeat (every stored entry contributes one term); those with a column
  * outside [0, vocab) or a value of -infinity count as not stored.  A row without stored entries has loss 0 and a gradient of zeros whatever its
  * logits are.  Logits of -infinity are columns of probability 0: they have a gradient of -p (0 where the teacher has nothing), and the loss is
- * +infinity where the teacher has p > 0.  A row of Z that holds nothing else, +infinity or not-a-number has a loss and a gradient that are not numbers.  inv_temperature must be positive and finite.
+ * +infinity where the teacher has p > 0.  A row of Z that holds nothing else, +infinity or not-a-number has a loss and a gradient that are not numbers.  inv_temperature must be positive and no more than 2.35e38.
  *
  * scorch_distill_loss writes loss[rows] and stats[rows][2], the largest logit of each row of Z and the sum of exp(x (z - largest));
  * scorch_distill_gradient takes these stats and writes dZ (rows x vocab, of Z's type), row i times dloss[i]; scorch_distill_loss_gradient does

@@ -64,8 +64,8 @@ static scorch_status_t check_distill(const char *call, int32_t rows, int32_t voc
         set_error("%s: negative dimension (rows=%d vocab=%d)", call, rows, vocab);
         return SCORCH_ERR_INVALID_ARG;
     }
-    if (!(x > 0.f) || !std::isfinite(x)) {
-        set_error("%s: inv_temperature = %g must be positive and finite", call, (double)x);
+    if (!(x > 0.f) || !std::isfinite(x * 1.44269504f)) {  // times log2(e): the kernels' powers are of two
+        set_error("%s: inv_temperature = %g must be positive and no more than 2.35e38", call, (double)x);
         return SCORCH_ERR_INVALID_ARG;
     }
     if (rows > 0 && !rowptr) {
