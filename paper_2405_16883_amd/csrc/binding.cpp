@@ -27,7 +27,15 @@ struct Args {
         if (!ok) return 0;
         const long long x = PyLong_AsLongLong(v[i]);
         if (x == -1 && PyErr_Occurred()) ok = false;
-        return (int32_t)x;
+        return narrow(x, "a size");
+    }
+    // What the C ABI takes in 32 bits.
+    int32_t narrow(int64_t x, const char *what) {
+        if (ok && (x < INT32_MIN || x > INT32_MAX)) {
+            PyErr_Format(PyExc_ValueError, "%s of %lld does not fit into 32 bits", what, (long long)x);
+            ok = false;
+        }
+        return ok ? (int32_t)x : 0;
     }
 
     // Device pointer of a tensor; nullptr for None and for a tensor without elements.
@@ -69,7 +77,10 @@ struct Args {
         }
         return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
     }
-    int32_t ld(int i, const char *name) { return (int32_t)wide_ld(i, name); }
+    int32_t ld(int i, const char *name) {
+        const int64_t x = wide_ld(i, name);
+        return ok && THPVariable_Unpack(v[i]).numel() > 0 ? narrow(x, "a row stride") : (int32_t)std::min<int64_t>(x, INT32_MAX);
+    }
 
     // A list of n int32 (or float) without gaps on the current device; n < 0: of any length, which is put there.  None: nullptr if that is
     // allowed.
@@ -264,7 +275,7 @@ PyObject *dense_layer(PyObject *, PyObject *const *v, Py_ssize_t nargs) {
         PyErr_SetString(PyExc_ValueError, "X, W, bias and Y do not fit together");
         return nullptr;
     }
-    const int32_t m = (int32_t)x.size(0), k = (int32_t)x.size(1), n = (int32_t)w.size(1);
+    const int32_t m = a.narrow(x.size(0), "a size"), k = a.narrow(x.size(1), "a size"), n = a.narrow(w.size(1), "a size");
     return status_of(a, [&] { return scorch_dense_layer(m, k, n, X, ldx, W, ldw, bias, act, Y, ldy, s); });
 }
 
