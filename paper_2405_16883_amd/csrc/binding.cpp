@@ -92,7 +92,7 @@ struct Args {
         const at::Tensor &t = THPVariable_Unpack(v[i]);
         if (!t.is_contiguous()) fail(PyExc_ValueError, "%s must be contiguous", name);
         else if (t.is_neg()) fail(PyExc_ValueError, "%s is a negated view", name);
-        else if (t.numel() > INT32_MAX) fail(PyExc_ValueError, "%s has too many elements", name);
+        else if (type != at::kByte && t.numel() > INT32_MAX) fail(PyExc_ValueError, "%s has too many elements", name);  // positions are int32
         else if (n >= 0 && t.numel() != n) PyErr_Format(PyExc_ValueError, "%s must have %lld elements, got %lld", name, (long long)n, (long long)t.numel()), ok = false;
         else if (t.get_device() != c10::hip::current_device()) fail(PyExc_ValueError, "%s must live on the current device", name);
         n = t.numel();
