@@ -319,7 +319,8 @@ def scorch_embedding_gradient(ids: torch.Tensor, dout: torch.Tensor, dE: torch.T
                               workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """dE[v] = scale * sum of the rows of dout whose id is v, or that added to dE.  ``workspace`` (uint8, GPU) is allocated with torch
     for the stream of the call if not given."""
-    if workspace is None and stream is not None:  # on the current stream the extension does it
+    # on the current stream the extension does it; it also refuses what has no rows and columns
+    if workspace is None and stream is not None and all(isinstance(t, torch.Tensor) and t.dim() == 2 for t in (dout, dE)):
         with torch.cuda.stream(stream):
             workspace = torch.empty(scorch_embedding_gradient_workspace_bytes(dout.shape[0], dE.shape[0], dE.shape[1]),
                                     dtype=torch.uint8, device=dE.device)
