@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kLogitsThreads, 8) void logits_kernel(const LogitsA
                     const int at = __builtin_ctz(b);
                     const float v = s.bias[j + at];
 #pragma unroll
-                    for (int i = 0; i < N; ++i) x[i] += i == at ? v : 0.f;
+                    for (int i = 0; i < N; ++i) x[i] = i == at ? x[i] + v : x[i];  // the others keep their bits
                 }
 #pragma unroll
             for (int i = 0; i < N; ++i)
