@@ -301,8 +301,10 @@ scorch_status_t scorch_embedding_lookup(int32_t tokens, int32_t vocab, int32_t d
 /*
  * Gradient of the table of a lookup:  dE[v, j] = scale * sum over t with ids[t] = v of dout[t, j], for every v < vocab (+0.0 for ids that do not
  * occur), or, with accumulate != 0, that added to what dE holds; rows of ids that do not occur are then neither read nor written.  The
- * token positions are sorted by id, so that a row of dE is the sum over a run of them, in ascending order; long runs are cut into pieces whose sums
- * are added in order.  dout: tokens x d, dE: vocab x d, of any two types; they must not overlap.  workspace (device, 256-byte aligned) of
+ * token positions are sorted by id, so that a row of dE is the sum over a run of them, added in ascending order.  Runs that reach far beyond
+ * one of the chunks into which the sorted list is cut have a sum per chunk; these are added in four groups (every fourth sum, ascending), the groups
+ * pairwise, and where a run has more than 32 of them, so for each of 16 equal shares, whose sums are added in ascending order.  All of it depends
+ * on the sizes and the ids only.  dout: tokens x d, dE: vocab x d, of any two types; they must not overlap.  workspace (device, 256-byte aligned) of
  * the size that the function after this one gives (host-only) holds the order and the pieces; executions that share one must not overlap in time.
  */
 scorch_status_t scorch_embedding_gradient(int32_t tokens, int32_t vocab, int32_t d, const int32_t *ids,
@@ -322,11 +324,13 @@ scorch_status_t scorch_embedding_gradient_workspace_bytes(int32_t tokens, int32_
  * Z: rows x vocab.  Entries of a row may be in any order and may repeat (every stored entry contributes one term); those with a column
  * outside [0, vocab) or a value of -infinity count as not stored.  A row without stored entries has loss 0 and a gradient of zeros whatever its
  * logits are.  Logits of -infinity are columns of probability 0: they have a gradient of -p (0 where the teacher has nothing), and the loss is
- * +infinity where the teacher has p > 0.  A row of Z that holds nothing else, +infinity or not-a-number has a loss and a gradient that are not numbers.  inv_temperature must be positive and no more than 2.35e38.
+ * +infinity where the teacher has p > 0 (in 32 bits: 2^-126 or more).  A row of Z that holds nothing else, +infinity or not-a-number has a loss and a gradient that are not numbers.  inv_temperature must be positive and no more than 2.35e38.
  *
  * scorch_distill_loss writes loss[rows] and stats[rows][2], the largest logit of each row of Z and the sum of exp(x (z - largest));
  * scorch_distill_gradient takes these stats and writes dZ (rows x vocab, of Z's type), row i times dloss[i]; scorch_distill_loss_gradient does
- * both at once, for a dloss known beforehand (a mean's 1 / rows, say).  dloss == NULL: ones.  dZ may be Z itself (with the same row
+ * both at once, for a dloss known beforehand (a mean's 1 / rows, say); it has a workgroup per row, so that for fewer than some 100 rows the two calls
+ * are the faster ones (one row of 131 072: 13 us against 20).  Columns that a row stores more than once cost the gradient a pass over the row's
+ * list for each such entry (2048 rows of 32 000 with 256 entries: 57 us, all of them pairs 99; with 1000: 86 and 765).  dloss == NULL: ones.  dZ may be Z itself (with the same row
  * stride) and must not overlap anything otherwise.  The gradient calls take up to SCORCH_DISTILL_VOCAB_MAX columns (SCORCH_ERR_UNSUPPORTED).
  */
 #define SCORCH_DISTILL_VOCAB_MAX 524288

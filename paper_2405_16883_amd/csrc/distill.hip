@@ -6,13 +6,14 @@
 // Bound by the bytes of the logits: the loss reads them once, the gradient reads and writes them.  A workgroup has a row.  Differences
 // from the largest logit are formed before they are scaled: nothing overflows where the result is a number.  Loss and gradient at once keep
 // the row in registers between the passes (maximum, sum, gradient), 16 or 20 vectors a thread with 16 wavefronts per CU: 81 920 16-bit columns, of
-// longer rows the rest is read again, mostly from the memory-side cache.  4096 rows of 131 072 bf16: 460 us, a copy of the same bytes 416; read
+// longer rows the rest is read again.  4096 rows of 131 072 bf16: 450 us, a copy of the same bytes 417; 1.42 times the logits come in from behind L2.  Read
 // again throughout 543; fewer vectors and 32 wavefronts 568; a row per CU, held whole by 1024 threads, 505.  8192 rows of 32 000: 205 us, the copy 201.
 // The loss alone reads 5.7 TB/s, the gradient alone moves 5.0.
 //
 // The gradient is dense, c (q_j - P_j), with P_j = 0 in all but the teacher's columns.  These are marked in a bitmap in LDS: a pass over the row
 // stores the others, vector by vector, and the threads that have the teacher's entries store theirs.  No element is written twice, so dZ
-// may be Z.  A second bitmap marks columns that the row stores more than once; their entries are then searched for and added in order.
+// may be Z.  A second bitmap marks columns that the row stores more than once; their entries are then searched for and added in order, a pass over
+// the list for each (2048 rows of 32 000, 1000 entries in pairs: 765 us, 86 if distinct).
 #include "device_util.h"
 #include "vocab_util.h"
 
@@ -345,7 +346,8 @@ template <typename T> static void launch_distill_gradient(DistillArgs a, hipStre
 }
 
 // The fewest threads whose registers hold the row, so that many rows are at work on a CU; with no more rows than CUs as many threads as a row takes
-// (256 rows of 131 072: 32 us, 512 threads 38).
+// (256 rows of 131 072: 32 us, 512 threads 38).  Rows are never cut here: 1 to 64 rows of 131 072 take 20 us, loss and gradient in two calls 13 to 17.
+// 512 threads with 20 vectors spill 5 registers and were the fastest of the forms tried for long rows all the same.
 template <typename T> static void launch_distill_both(const DistillArgs &a, hipStream_t stream) {
     constexpr int kBoth = kDistillLoss | kDistillGradient;
     constexpr int64_t kPer = 16 / sizeof(T);

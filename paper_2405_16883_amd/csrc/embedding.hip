@@ -2,16 +2,16 @@
 //
 // Lookup: out[t, :] = scale E[ids[t], :].  A copy with a gather in front: bound by the bytes of the rows read and written.  A group of
 // lanes takes a row, 16 bytes of the wider type per lane and step, and several rows at a time, so that their loads are in flight together.
-// 16 384 rows of 4096 from a 32-bit table of 131 072 to 16 bits: 52 us, 4.8 TB/s (a large copy reaches as much); 50 021 odd rows of 1001: 25 us, 36 us
-// when nothing of the table is in a cache.
+// 16 384 rows of 4096 from a 32-bit table of 131 072 to 16 bits: 58 us, 4.2 TB/s (a large copy: 4.76), 53 us with the same ids again; 50 021 odd rows
+// of 1001: 36 us and 25.
 //
 // Gradient: dE[v, :] = scale * sum of the rows dout[t, :] with ids[t] = v.  Bound by the bytes of dout and dE.  Few ids make up much of a
 // text, so rows of dE differ in work by orders of magnitude: the token positions are sorted by id and the sorted list is cut into chunks
 // of equal length, whatever the runs in it.  A wavefront walks a chunk of a tile of columns with the sum of the current run in registers, and
-// a little beyond it, to finish a run; what reaches further leaves partial rows, which a last launch adds in order.  No floating-point
-// atomics: the order of every sum is fixed.  16 384 tokens added to 131 072 x 4096: sort 17, sums 66 (5.5 TB/s, some of it from caches), partial rows 9 us;
-// 262 144 tokens, 50 257 x 768 overwritten: 30, 131 (3.9 TB/s), 12 us.  What is left there: half of the second tile of columns is empty, and the tail's
-// wavefronts store a row per token.
+// a little beyond it, to finish a run; what reaches further leaves partial rows, which a last launch adds up.  No floating-point
+// atomics: the order of every sum is fixed, ascending within a chunk, in four interleaved groups over partial rows.  16 384 tokens added to
+// 131 072 x 4096: sort 18, sums 66 (5.5 TB/s, with the same inputs again), partial rows 9 us; 262 144 tokens, 50 257 x 768 overwritten: 31, 131 (3.9 TB/s),
+// 12 us.  What is left there: half of the second tile of columns is empty, and the tail's wavefronts store a row per token.
 #include "device_util.h"
 #include "vocab_util.h"
 
@@ -544,7 +544,7 @@ __global__ __launch_bounds__(kBlock) void run_sum_kernel(const RunArgs a) {
     if (!FEW && tail_here && unit % a.tiles == 0 && lane == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1)] = (int32_t)c;
 }
 
-// Adds up the runs that have partial rows, which are listed in any order.  A wavefront takes a run and 64 columns, 16 lanes a row, so that 32 rows are
+// Adds up the runs that have partial rows; the list of these runs is in any order, what is added to what is not.  A wavefront takes a run and 64 columns, 16 lanes a row, so that 32 rows are
 // in flight; if the run has more, the wavefronts of the workgroup share it, in equal consecutive shares.
 constexpr int kJoinThreads = 1024;
 constexpr int kJoinWaves = kJoinThreads / kWave;

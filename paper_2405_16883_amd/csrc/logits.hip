@@ -5,8 +5,10 @@
 // each token occurs in the row's history and looks the biases up there, with the tile's logits already on their way to registers; then it passes
 // over the tile once.  Counts are whole numbers, so the order of the atomic additions changes nothing.  Where a column has several biases, they are
 // added up in the order of the list.  256 rows of 131 072, bf16 to f32, histories of 2048, 64 biases, mask: 43 us, 57 when nothing is in a cache (a
-// plain copy 29 and 43); without biases 35.  33 rows of 50 257 with histories of 32 768 and 300 biases: 22 us, of which 12 go into biases
-// that repeat a token and 4 into the history, both on the one CU that has the row's most frequent tokens.
+// plain copy 29 and 43); without biases 35.  33 rows of 50 257 with histories of 32 768 and 300 biases: 21 us, of which 8 go into biases
+// that repeat a token and 4 into the history, both on the one CU that has the row's most frequent tokens; with distinct biases 12.5.
+// From 16 to 16 bits a vector has 8 columns and a tile 16 384: LDS has room for one workgroup per CU if there are biases (80 KB, 144 KB with a history),
+// and the same batch takes 46 us where a copy takes 20.  64 registers, for two workgroups per CU, are up to 10 too few; no form without spills was measured.
 #include "device_util.h"
 #include "vocab_util.h"
 
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(kLogitsThreads, 8) void logits_kernel(const LogitsA
     }
 }
 
-// Workgroups per row: those that take the fewest rounds of 2 per CU times tiles, counting a tile for a workgroup's start.  256 rows of 16 tiles: 2 parts 57 us,
+// Workgroups per row: those that take the fewest rounds of 2 per CU times tiles, counting a tile for a workgroup's start (2 also where LDS has room for one).  256 rows of 16 tiles: 2 parts 57 us,
 // 4 60, 8 63, 16 68.
 static int32_t row_parts(int32_t rows, int32_t tiles) {
     const int64_t slots = 2 * kCus;
