@@ -145,6 +145,13 @@ def _check(status: int) -> None:
         raise ScorchError(status, f"{lib.scorch_status_string(status).decode()}: {lib.scorch_last_error().decode()}")
 
 
+def _fit_32_bits(*sizes: int) -> None:
+    """ctypes takes integers modulo 2^32."""
+    for x in sizes:
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"a size of {x} does not fit into 32 bits")
+
+
 def _dev_ptr(t: Optional[torch.Tensor], dtype: torch.dtype, name: str) -> Optional[int]:
     if t is None:
         return None
@@ -181,6 +188,7 @@ def scorch_spmm_csr_static(m: int, k: int, n: int, rowptr: torch.Tensor, colidx:
 
 
 def scorch_spmm_plan_workspace_bytes(m: int, k: int, n: int, nnz: int) -> int:
+    _fit_32_bits(m, k, n)
     lib = load_library()
     out = ctypes.c_size_t(0)
     _check(lib.scorch_spmm_plan_workspace_bytes(m, k, n, nnz, ctypes.byref(out)))
@@ -223,6 +231,7 @@ def scorch_spmm_plan(m: int, k: int, n: int, rowptr: torch.Tensor, nnz: int,
                      stream: Optional[torch.cuda.Stream] = None) -> SpmmPlan:
     """Analyse the pattern behind ``rowptr`` (and, if given, ``colidx``).  ``workspace`` (uint8, GPU) is allocated
     with torch if not given."""
+    _fit_32_bits(m, k, n)
     lib = load_library()
     if workspace is None:
         workspace = torch.empty(scorch_spmm_plan_workspace_bytes(m, k, n, nnz), dtype=torch.uint8, device=rowptr.device)
@@ -293,6 +302,7 @@ def scorch_dcsr_to_csr_rowptr(m: int, row_ids: torch.Tensor, row_pos: torch.Tens
                               bad_flag: Optional[torch.Tensor] = None,
                               stream: Optional[torch.cuda.Stream] = None) -> None:
     """CSR row pointers of a doubly compressed matrix given the ids of its stored rows and their entry ranges."""
+    _fit_32_bits(m)
     lib = load_library()
     if rowptr_out.numel() != m + 1 or row_pos.numel() != row_ids.numel() + 1:
         raise ValueError("rowptr_out needs m + 1 entries and row_pos one more entry than row_ids")
@@ -310,6 +320,7 @@ def scorch_embedding_lookup(ids: torch.Tensor, E: torch.Tensor, out: torch.Tenso
 
 
 def scorch_embedding_gradient_workspace_bytes(tokens: int, vocab: int, d: int) -> int:
+    _fit_32_bits(tokens, vocab, d)
     out = ctypes.c_size_t(0)
     _check(load_library().scorch_embedding_gradient_workspace_bytes(tokens, vocab, d, ctypes.byref(out)))
     return int(out.value)
